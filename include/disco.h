@@ -450,6 +450,94 @@ int disco_prefill(const disco_model* m, disco_kv* kv, const int32_t* dev_tokens,
 int disco_prefill_ex(const disco_model* m, disco_kv* kv, const int32_t* dev_tokens, int n_tokens,
                      float* dev_logits_last, unsigned flags, void* dev_ws, size_t ws_bytes, disco_stream s);
 
+/* ---- several sequences that continue one prompt ----------------------------------------------- */
+
+/* Beams of a beam search, parallel samples, several candidate blocks: sequences that share a prompt and then go their own
+ * ways.  The prompt's keys and values are held once (in a disco_kv or any pool of pages), every
+ * sequence's own positions in pages that a table per sequence names.  The calls of a decoding step, per layer:
+ * disco_append (keys and values of the new tokens into the cache, queries out), disco_attn_shared (attention); then
+ * once a step disco_beam_select (next tokens) and disco_beam_reorder (page tables).  Calls with no rows return 0 and do
+ * nothing.  Nothing here allocates or keeps state, so a step may be captured into a graph; calls that run at the same time
+ * need workspaces of their own.                                                                                          */
+
+enum { DISCO_F32 = 0, DISCO_BF16 = 1 };   /* element types of activations */
+
+/* One layer of such a cache.  Page layout as in disco_kv_create: [K | V][kv head] blocks of page_tokens x d_head bf16, K blocks
+ * [token][d_head], V blocks [d_head][token]; page_tokens a multiple of 4, d_head 64 or 128.  The position of a sequence's own
+ * entry p is prefix_len + p.                                                                                             */
+typedef struct disco_shared_kv {
+  const void* dev_prefix;             /* the prompt's pages of this layer, 16-byte aligned; unused if prefix_len == 0      */
+  const int32_t* dev_prefix_table;    /* physical page of prompt page i; NULL: page i                                      */
+  int32_t n_prefix_pages;             /* pages in that pool                                                                */
+  int32_t prefix_len;                 /* positions of the prompt                                                           */
+  void* dev_pages;                    /* the sequences' own pages of this layer, 16-byte aligned                            */
+  const int32_t* dev_tables;          /* [n_seqs][table_ld]: physical pages of a sequence's positions                       */
+  const int32_t* dev_lens;            /* [n_seqs]: own positions, those of the tokens being processed included              */
+  int32_t n_pages;                    /* pages in the pool at dev_pages                                                    */
+  int32_t table_ld;                   /* pages a table holds                                                               */
+  int32_t n_seqs;
+  int32_t page_tokens, n_kv_heads, d_head;
+} disco_shared_kv;
+
+/* (cos, sin) of every position and channel pair, fp32 [n_pos][d_head / 2][2]: angle pos * base^(-2 i / d_head), formed in 64 bits. */
+int disco_rope_table(float* dev_table, int n_pos, int d_head, float base, disco_stream s);
+
+/* Appends the keys and values of n_rows rows and writes their queries.  Row i of dev_qkv holds [q heads | k heads | v heads]
+ * (n_heads + 2 n_kv_heads heads of d_head, element type dtype, row stride ld_qkv).  With dev_seq and dev_pos (both or neither),
+ * row i is own position dev_pos[i] of sequence dev_seq[i], in any order; without them n_rows is a multiple T of n_seqs and row i
+ * is token i % T of sequence i / T, at own position dev_lens[seq] - T + i % T.
+ * dev_q_gain, dev_k_gain (fp32 [d_head], either may be NULL: none): query and key heads are normalised first,
+ * x * gain / sqrt(mean(x^2) + eps).  dev_rope (NULL: no rotation): table of disco_rope_table with n_rope positions, which has to
+ * cover prefix_len + table_ld * page_tokens (DISCO_ECAP); queries and keys are rotated, channel c with c + d_head / 2, by the angle of
+ * position prefix_len + own position.  Norm and rotation are fp32; cache entries are rounded to bf16 once, queries to dtype.
+ * A row whose sequence is outside [0, n_seqs) or whose position is outside its table is padding: nothing of it is written.  A row
+ * whose page is outside [0, n_pages) has its query written and no cache entry.  Rows of one call that name the same sequence and position leave either row's values
+ * there, and maybe some of each.  dev_q: [n_rows][n_heads * d_head], row stride ld_q; it may not overlap dev_qkv.  Row starts are 16-byte aligned.      */
+int disco_append(const disco_shared_kv* kv, const void* dev_qkv, int dtype, int64_t ld_qkv, int n_rows, int n_heads,
+                 const int32_t* dev_seq, const int32_t* dev_pos, const float* dev_rope, int n_rope,
+                 const float* dev_q_gain, const float* dev_k_gain, float eps, void* dev_q, int64_t ld_q, disco_stream s);
+
+/* Attention of n_tok tokens (1 .. DISCO_MAX_BLOCK) of every sequence: row seq * n_tok + t of dev_q sees the whole prompt and its sequence's
+ * own positions below dev_lens[seq] - n_tok + 1 + t.  out = softmax(scale q . k) v per query head; query head h reads K / V head
+ * h / (n_heads / n_kv_heads).  dev_lse (may be NULL): fp32 [rows][n_heads], the natural logarithm of the sum of exponentials.
+ * A row that sees nothing has output 0 and dev_lse -inf.  What a row does not see does not touch it, infinities and NaN included.
+ * A page id outside its pool is not read; rows that would have seen it come out as NaN.
+ * The prompt's pages are read once for all sequences.  Sums and statistics are fp32.  DISCO_F32 queries: products of three bf16 terms a
+ * factor (24 bits); DISCO_BF16: probabilities are rounded to bf16 before the product with V.
+ * max_len: the largest value expected in dev_lens (0: what a table holds).  It only shapes the launch: longer sequences are right too, and slower.
+ * dev_ws: disco_attn_shared_bytes(kv, n_tok, n_heads, max_len) bytes of the same arguments, 256-byte aligned, contents irrelevant.
+ * dev_out may not overlap dev_q; row starts are 16-byte aligned.                                                                         */
+size_t disco_attn_shared_bytes(const disco_shared_kv* kv, int n_tok, int n_heads, int max_len);
+int disco_attn_shared(const disco_shared_kv* kv, const void* dev_q, int dtype, int64_t ld_q, int n_tok, int n_heads, float scale,
+                      void* dev_out, int64_t ld_out, float* dev_lse, int max_len, void* dev_ws, size_t ws_bytes, disco_stream s);
+
+/* Beam search's choice: of the candidates (beam b, token v) of a group of n_beams rows, the k with the largest
+ * dev_scores[b] + logits[b][v] - logsumexp(logits[b]), in descending order, equal ones by the lower b, then the lower v.  Keys are compared in
+ * 64 bits; dev_scores_out holds them in fp32.  A finished beam (dev_done[b] != 0; dev_done may be NULL) is one candidate:
+ * end_token with its score as it is.  dev_tokens, dev_parents (b, inside the group), dev_scores_out, dev_done_out (may be NULL; 1 if the parent
+ * was finished or the token is end_token; end_token -1: no token ends a sequence) are [n_groups][k].  Candidates of probability zero (logit
+ * or score -inf) are never taken; places left over hold token -1, parent -1, score -inf, done 1.  A logit that is NaN or +inf (in a beam
+ * that is not finished), or such a score, makes the whole group token -1, parent -1, score NaN, done 1.
+ * dev_logits: rows of vocab, row stride ld_logits >= vocab elements, any element alignment.                                                  */
+#define DISCO_MAX_BEAMS 64
+#define DISCO_BEAM_MAX_K 128
+#define DISCO_BEAM_MAX_VOCAB 1048576
+size_t disco_beam_select_bytes(int n_groups, int n_beams, int vocab, int k);
+int disco_beam_select(const void* dev_logits, int dtype, int64_t ld_logits, int n_groups, int n_beams, int vocab, int k,
+                      const float* dev_scores, const int32_t* dev_done, int end_token, int32_t* dev_tokens, int32_t* dev_parents,
+                      float* dev_scores_out, int32_t* dev_done_out, void* dev_ws, size_t ws_bytes, disco_stream s);
+
+/* Makes sequence b of every group of n_beams go on from sequence dev_parents[b] of its group (outside [0, n_beams): from itself).  All
+ * hold len own positions.  dev_tables_out[b] gets the parent's entries for the full pages (shared by reference: full pages are not written
+ * again), and beyond the page being filled its own.  For the page being filled (len % page_tokens != 0) the parent's first child takes over the
+ * page, and every further child the page of a sequence without a child, in order of both, with the contents copied in all n_layers layers
+ * (layer l at dev_pages + l * layer_stride elements; a page is page_elems = 2 n_kv_heads page_tokens d_head consecutive elements).
+ * The pages that the group's tables hold for this place and beyond must be distinct.  A page id outside [0, n_pages) is passed on and
+ * not copied.  dev_tables_out may not overlap dev_tables.                                                                               */
+int disco_beam_reorder(void* dev_pages, int n_layers, int64_t layer_stride, int n_pages, int64_t page_elems, const int32_t* dev_tables,
+                       int32_t* dev_tables_out, int table_ld, const int32_t* dev_parents, int n_groups, int n_beams, int len,
+                       int page_tokens, disco_stream s);
+
 /* ---- launch structure ------------------------------------------------------------------------------ */
 
 /* How a forward is cut into launches.  Process-wide; returns the previous mode, or DISCO_EINVAL.  Not to be

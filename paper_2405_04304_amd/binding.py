@@ -75,6 +75,12 @@ class IterResult(C.Structure):
                 ("draft_steps_enqueued", C.c_int32), ("block", C.c_int32 * MAX_BLOCK), ("emit", C.c_int32 * MAX_BLOCK)]
 
 
+class SharedKVDesc(C.Structure):
+    _fields_ = [("dev_prefix", C.c_void_p), ("dev_prefix_table", C.c_void_p), ("n_prefix_pages", C.c_int32), ("prefix_len", C.c_int32),
+                ("dev_pages", C.c_void_p), ("dev_tables", C.c_void_p), ("dev_lens", C.c_void_p), ("n_pages", C.c_int32),
+                ("table_ld", C.c_int32), ("n_seqs", C.c_int32), ("page_tokens", C.c_int32), ("n_kv_heads", C.c_int32), ("d_head", C.c_int32)]
+
+
 _SIGNATURES = {
     "disco_last_error": (C.c_char_p, []),
     "disco_pack_weight": (C.c_int, [C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p]),
@@ -132,6 +138,17 @@ _SIGNATURES = {
     "disco_clf_eval": (C.c_int, [C.POINTER(Clf), C.c_void_p, C.c_void_p, C.c_int, C.c_float, C.c_void_p,
                                  C.c_void_p, C.c_void_p]),
     "disco_set_launch_mode": (C.c_int, [C.c_int]),
+    "disco_rope_table": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_float, C.c_void_p]),
+    "disco_append": (C.c_int, [C.POINTER(SharedKVDesc), C.c_void_p, C.c_int, C.c_int64, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p,
+                               C.c_int, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_int64, C.c_void_p]),
+    "disco_attn_shared_bytes": (C.c_size_t, [C.POINTER(SharedKVDesc), C.c_int, C.c_int, C.c_int]),
+    "disco_attn_shared": (C.c_int, [C.POINTER(SharedKVDesc), C.c_void_p, C.c_int, C.c_int64, C.c_int, C.c_int, C.c_float, C.c_void_p, C.c_int64,
+                                    C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "disco_beam_select_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int, C.c_int]),
+    "disco_beam_select": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_int,
+                                    C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "disco_beam_reorder": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_int, C.c_int64, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int,
+                                     C.c_int, C.c_int, C.c_int, C.c_void_p]),
     "disco_clf_examples": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
     "disco_heuristic_next": (C.c_int, [C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int]),
     "disco_probe_enable": (C.c_int, [C.c_int]),
@@ -308,6 +325,147 @@ def disco_draft_loop_sampled(model, kv, clf, tokens_in, n_in, cap, static_sl, po
                                           _ptr(u_draft), _ptr(draft_probs), _ptr(logits), _ptr(steps), _ptr(out),
                                           _ptr(host_out), _ptr(ws.buf), ws.nbytes,
                                           _stream() if stream is None else stream))
+
+
+# ---- several sequences that continue one prompt ------------------------------------------------
+
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise DiscoError(EINVAL, what)
+
+
+def _tensor(t, what: str, dtype=None, numel: Optional[int] = None, optional: bool = False):
+    """Checks what the library cannot see of a tensor: where it lives, its type, that it is contiguous, its size."""
+    if t is None:
+        _need(optional, f"{what} is missing")
+        return
+    _need(t.is_cuda and t.device.index == torch.cuda.current_device(), f"{what} is not on the current device")
+    _need(dtype is None or t.dtype == dtype, f"{what} has type {t.dtype}, not {dtype}")
+    _need(t.is_contiguous(), f"{what} is not contiguous")
+    _need(numel is None or t.numel() >= numel, f"{what} has {t.numel()} elements, {numel} needed")
+
+
+def _rows(t, what: str, n: int, width: int):
+    """(element type code, row stride) of a matrix of n rows whose columns are contiguous."""
+    _need(t.is_cuda and t.device.index == torch.cuda.current_device(), f"{what} is not on the current device")
+    _need(t.dtype in _DTYPES, f"{what} has type {t.dtype}: float32 or bfloat16")
+    _need(t.dim() == 2 and t.shape[0] >= n and t.shape[1] >= width, f"{what} has shape {tuple(t.shape)}, ({n}, {width}) needed")
+    _need(t.stride(1) == 1 or t.shape[1] == 1, f"{what}: the elements of a row are not contiguous")
+    return _DTYPES[t.dtype], max(t.stride(0), width) if n < 2 else t.stride(0)
+
+
+class SharedKV:
+    """One layer of the paged cache of several sequences behind one prompt (disco_shared_kv); keeps its tensors alive.
+
+    pages, prefix_pages: bf16 [pages, 2, n_kv_heads, page_tokens * d_head]; tables: int32 [n_seqs, pages a table holds]; lens: int32
+    [n_seqs] (None if every append names its rows' positions); prefix_table: int32 or None (page i of the prompt is page i)."""
+
+    def __init__(self, pages, tables, lens, page_tokens: int, n_kv_heads: int, d_head: int, prefix_pages=None, prefix_len: int = 0,
+                 prefix_table=None):
+        page_shape = (2, n_kv_heads, page_tokens * d_head)
+        _tensor(pages, "pages", torch.bfloat16)
+        _need(pages.dim() == 4 and tuple(pages.shape[1:]) == page_shape, f"pages have shape {tuple(pages.shape)}, (pages, {page_shape}) needed")
+        _tensor(tables, "tables", torch.int32)
+        _need(tables.dim() == 2, "tables: [sequences, pages]")
+        _tensor(lens, "lens", torch.int32, tables.shape[0], optional=True)
+        n_prefix = 0
+        if prefix_pages is not None:
+            _tensor(prefix_pages, "prefix_pages", torch.bfloat16)
+            _need(prefix_pages.dim() == 4 and tuple(prefix_pages.shape[1:]) == page_shape, "prefix_pages have another page shape")
+            n_prefix = prefix_pages.shape[0]
+            _tensor(prefix_table, "prefix_table", torch.int32, -(-prefix_len // page_tokens), optional=True)
+        self._keep = (pages, tables, lens, prefix_pages, prefix_table)
+        self.lens = lens
+        self.n_seqs, self.n_kv_heads, self.d_head = tables.shape[0], n_kv_heads, d_head
+        self.c = SharedKVDesc(_ptr(prefix_pages), _ptr(prefix_table), n_prefix, prefix_len, _ptr(pages), _ptr(tables), _ptr(lens),
+                              pages.shape[0], tables.shape[1], tables.shape[0], page_tokens, n_kv_heads, d_head)
+
+
+def disco_rope_table(n_pos: int, d_head: int, base: float = 10000.0, device="cuda", stream=None) -> torch.Tensor:
+    """fp32 [n_pos, d_head / 2, 2]: (cos, sin) of every position and channel pair."""
+    t = torch.empty(n_pos, d_head // 2, 2, dtype=torch.float32, device=device)
+    _check(lib().disco_rope_table(_ptr(t), n_pos, d_head, base, _stream() if stream is None else stream))
+    return t
+
+
+def disco_append(kv: SharedKV, qkv, n_heads: int, q, seq=None, pos=None, rope=None, q_gain=None, k_gain=None, eps: float = 1e-6,
+                 stream=None):
+    """Keys and values of the rows of qkv into the cache, queries (normalised, rotated) to q."""
+    n, d = qkv.shape[0], kv.d_head
+    code, ld = _rows(qkv, "qkv", n, (n_heads + 2 * kv.n_kv_heads) * d)
+    code_q, ld_q = _rows(q, "q", n, n_heads * d)
+    _need(code == code_q, "q has another type than qkv")
+    for t, what in ((seq, "seq"), (pos, "pos")):
+        _tensor(t, what, torch.int32, n, optional=True)
+    _tensor(rope, "rope", torch.float32, optional=True)
+    _need(rope is None or (rope.dim() == 3 and tuple(rope.shape[1:]) == (d // 2, 2)), f"rope: [positions, {d // 2}, 2]")
+    for t, what in ((q_gain, "q_gain"), (k_gain, "k_gain")):
+        _tensor(t, what, torch.float32, d, optional=True)
+    _check(lib().disco_append(C.byref(kv.c), _ptr(qkv), code, ld, n, n_heads, _ptr(seq), _ptr(pos), _ptr(rope),
+                              rope.shape[0] if rope is not None else 0, _ptr(q_gain), _ptr(k_gain), eps, _ptr(q), ld_q,
+                              _stream() if stream is None else stream))
+
+
+def disco_attn_shared_bytes(kv: SharedKV, n_tok: int, n_heads: int, max_len: int = 0) -> int:
+    n = lib().disco_attn_shared_bytes(C.byref(kv.c), n_tok, n_heads, max_len)
+    if n == 0:
+        raise DiscoError(EINVAL, last_error())
+    return n
+
+
+def disco_attn_shared(kv: SharedKV, q, n_tok: int, n_heads: int, out, ws, lse=None, scale: Optional[float] = None, max_len: int = 0,
+                      stream=None):
+    """Attention of n_tok tokens of every sequence; ws: uint8, disco_attn_shared_bytes of the same arguments.  scale: d_head ** -0.5."""
+    n = kv.n_seqs * n_tok
+    code, ld = _rows(q, "q", n, n_heads * kv.d_head)
+    code_o, ld_o = _rows(out, "out", n, n_heads * kv.d_head)
+    _need(code == code_o, "out has another type than q")
+    _tensor(lse, "lse", torch.float32, n * n_heads, optional=True)
+    _tensor(ws, "ws", torch.uint8)
+    _need(kv.lens is not None or n == 0, "the cache has no lens")
+    _check(lib().disco_attn_shared(C.byref(kv.c), _ptr(q), code, ld, n_tok, n_heads, kv.d_head ** -0.5 if scale is None else scale, _ptr(out),
+                                   ld_o, _ptr(lse), max_len, _ptr(ws), ws.numel(), _stream() if stream is None else stream))
+
+
+def disco_beam_select_bytes(n_groups: int, n_beams: int, vocab: int, k: int) -> int:
+    n = lib().disco_beam_select_bytes(n_groups, n_beams, vocab, k)
+    if n == 0:
+        raise DiscoError(EINVAL, last_error())
+    return n
+
+
+def disco_beam_select(logits, scores, n_groups: int, n_beams: int, k: int, tokens, parents, scores_out, ws, done=None, done_out=None,
+                      end_token: int = -1, stream=None):
+    """The k best (beam, token) of every group; logits: [n_groups * n_beams, vocab]."""
+    n, vocab = n_groups * n_beams, logits.shape[1] if logits.dim() == 2 else 0
+    code, ld = _rows(logits, "logits", n, vocab)
+    _tensor(scores, "scores", torch.float32, n)
+    _tensor(done, "done", torch.int32, n, optional=True)
+    for t, what, dtype in ((tokens, "tokens", torch.int32), (parents, "parents", torch.int32), (scores_out, "scores_out", torch.float32)):
+        _tensor(t, what, dtype, n_groups * k)
+    _tensor(done_out, "done_out", torch.int32, n_groups * k, optional=True)
+    _tensor(ws, "ws", torch.uint8)
+    _check(lib().disco_beam_select(_ptr(logits), code, ld, n_groups, n_beams, vocab, k, _ptr(scores), _ptr(done), end_token, _ptr(tokens),
+                                   _ptr(parents), _ptr(scores_out), _ptr(done_out), _ptr(ws), ws.numel(),
+                                   _stream() if stream is None else stream))
+
+
+def disco_beam_reorder(pages, tables, parents, tables_out, n_groups: int, n_beams: int, length: int, page_tokens: int, stream=None):
+    """Sequence b goes on from parents[b]; pages: bf16 [layers, pages, 2, n_kv_heads, page_tokens * d_head], layers may be strided."""
+    _need(pages.is_cuda and pages.device.index == torch.cuda.current_device(), "pages are not on the current device")
+    _need(pages.dim() == 5 and pages.dtype == torch.bfloat16 and pages.shape[0] > 0 and pages.shape[2] == 2 and pages[0].is_contiguous(),
+          "pages: bfloat16 [layers, pages, 2, K / V heads, page_tokens * d_head], a layer contiguous")
+    _need(pages.shape[4] % page_tokens == 0, "pages have another page size")
+    _tensor(tables, "tables", torch.int32)
+    _need(tables.dim() == 2 and tables.shape[0] >= n_groups * n_beams, "tables: [sequences, pages]")
+    _tensor(parents, "parents", torch.int32, n_groups * n_beams)
+    _tensor(tables_out, "tables_out", torch.int32, tables.numel())
+    _check(lib().disco_beam_reorder(_ptr(pages), pages.shape[0], pages.stride(0), pages.shape[1], pages[0, 0].numel(), _ptr(tables),
+                                    _ptr(tables_out), tables.shape[1], _ptr(parents), n_groups, n_beams, length, page_tokens,
+                                    _stream() if stream is None else stream))
 
 
 TRAIN_MAX_N = 2560

@@ -6,7 +6,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdisco.so")
-SOURCES = ["disco_kernels.hip", "disco_api.cpp"]
+SOURCES = ["disco_kernels.hip", "disco_shared.hip", "disco_api.cpp", "disco_shared_api.cpp"]
 
 
 def build(verbose: bool = True) -> str:

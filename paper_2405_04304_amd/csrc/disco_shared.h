@@ -1,0 +1,65 @@
+// Launcher interface between the boundary of the operators for several sequences behind one prompt (disco_shared_api.cpp) and
+// their gfx950 kernels (disco_shared.hip).  Nothing here is exported.
+#pragma once
+#include "disco_internal.h"
+
+namespace disco {
+
+// One layer of the paged cache: the prompt's pages and every sequence's own.  Page: [K | V][kv head] blocks of pt x dh bf16, K blocks
+// [token][channel], V blocks [channel][token].
+struct SharedKv {
+  const bf16_t* prefix; const int32_t* prefix_table; int n_prefix_pages, prefix_len;
+  bf16_t* pages; const int32_t* tables; const int32_t* lens; int n_pages, table_ld, n_seqs;
+  int pt, nkv, dh;
+  int pt_shift;                      // log2 of pt, or -1
+};
+
+struct AppendArgs {
+  SharedKv kv;
+  const void* qkv; int64_t ld; int rows, nq;
+  const int32_t* seq; const int32_t* pos;
+  int n_tok;                         // seq == nullptr: row i is token i % n_tok of sequence i / n_tok
+  const float* rope;
+  const float* q_gain; const float* k_gain; float eps;
+  void* q; int64_t ld_q;
+};
+hipError_t launch_append(const AppendArgs& a, bool fp32, hipStream_t s);
+
+// Ranges and launches of an attention call.
+struct SharedAttnPlan {
+  int wr_prefix;                     // 32-row wavefronts of a workgroup over the prompt's positions (0: no prompt)
+  int prefix_tiles, prefix_splits, prefix_len;    // row tiles of a kv head, ranges, positions of a range
+  int wr_own, own_tiles, own_splits, own_len;
+  int parts;                         // partial results of a row
+  size_t bytes;                      // of the partial results (0 with one part)
+};
+SharedAttnPlan shared_attn_plan(int n_seqs, int n_tok, int nq, int nkv, int dh, int prefix_len, int max_len);
+
+struct SharedAttnArgs {
+  SharedKv kv;
+  const void* q; int64_t ld_q; int n_tok, nq; float scale;
+  void* out; int64_t ld_out; float* lse;
+  float* part; float2* ml;           // [part][kv head][row][channel] and their (maximum in log2 units, sum)
+  SharedAttnPlan plan;
+};
+hipError_t launch_shared_attn(const SharedAttnArgs& a, bool fp32, hipStream_t s);
+
+constexpr int BEAM_CHUNK = 4096;     // logits of a workgroup
+struct BeamSelectArgs {
+  const void* logits; int64_t ld; int n_groups, n_beams, vocab, k;
+  const float* scores; const int32_t* done; int end_token;
+  int32_t* tokens; int32_t* parents; float* scores_out; int32_t* done_out;
+  float2* stats;                     // [row][chunk]: maximum, sum of exponentials
+  unsigned long long* cand;          // [row][chunk][k]
+  int chunks;
+};
+hipError_t launch_beam_select(const BeamSelectArgs& a, bool fp32, hipStream_t s);
+
+struct BeamReorderArgs {
+  bf16_t* pages; int n_layers; int64_t layer_stride; int n_pages; int64_t page_elems;
+  const int32_t* tables; int32_t* tables_out; int table_ld; const int32_t* parents;
+  int n_groups, n_beams, full, live;
+};
+hipError_t launch_beam_reorder(const BeamReorderArgs& a, hipStream_t s);
+
+}  // namespace disco

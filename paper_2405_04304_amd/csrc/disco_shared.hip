@@ -1,0 +1,720 @@
+// gfx950 (MI355X) kernels for several sequences that continue one prompt: keys and values appended to a paged cache with head
+// norms and rotation on the way, attention that reads the prompt's pages once for all sequences, the beams' next tokens, and
+// the reordering of their page tables.
+#include "disco_device.h"
+#include "disco_shared.h"
+
+namespace disco {
+
+namespace {
+
+constexpr float LOG2E = 1.44269504088896f, LN2 = 0.693147180559945f;
+
+__device__ __forceinline__ int page_of(const SharedKv& kv, int pos) { return kv.pt_shift >= 0 ? pos >> kv.pt_shift : pos / kv.pt; }
+
+// Four consecutive elements of a row as floats, and back.
+__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 load4(const bf16_t* p) {
+  const uint2 u = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
+}
+__device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+__device__ __forceinline__ void store4(bf16_t* p, float4 v) { *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)); }
+
+// ---------------------------------------------------------------------------------------------
+// append
+// ---------------------------------------------------------------------------------------------
+
+// Where row i goes: its sequence's own position and the page that holds it; pos < 0: nowhere (padding, or outside the tables).
+struct RowPlace { int seq, pos, page; };
+__device__ __forceinline__ RowPlace row_place(const AppendArgs& a, int i) {
+  RowPlace r{-1, -1, -1};
+  if (i >= a.rows) return r;
+  if (a.seq != nullptr) {
+    r.seq = a.seq[i];
+    r.pos = a.pos[i];
+  } else {
+    r.seq = i / a.n_tok;
+    r.pos = a.kv.lens[r.seq] - a.n_tok + (i - r.seq * a.n_tok);
+  }
+  if ((unsigned)r.seq >= (unsigned)a.kv.n_seqs || r.pos < 0 || page_of(a.kv, r.pos) >= a.kv.table_ld) { r.seq = r.pos = -1; return r; }
+  r.page = a.kv.tables[(size_t)r.seq * a.kv.table_ld + page_of(a.kv, r.pos)];
+  if ((unsigned)r.page >= (unsigned)a.kv.n_pages) r.page = -1;
+  return r;
+}
+
+// y_h = rotate(norm(x_h)) for query and key heads, v as it is.  DH / 8 lanes hold a head of a row: four channels of the first half and
+// their rotary partners in the second.
+template <int DH, typename T>
+__global__ __launch_bounds__(256) void k_append(AppendArgs a) {
+  constexpr int LPR = DH / 8, RPW = 256 / LPR;
+  const int i = blockIdx.x * RPW + threadIdx.x / LPR, c = (threadIdx.x % LPR) * 4, h = blockIdx.y;
+  const RowPlace at = row_place(a, i);
+  if (at.pos < 0) return;
+  const SharedKv& kv = a.kv;
+  const T* x = static_cast<const T*>(a.qkv) + (size_t)i * a.ld + (size_t)h * DH;
+  float4 lo = load4(x + c), hi = load4(x + DH / 2 + c);
+  const int off = at.pos - page_of(kv, at.pos) * kv.pt;
+  if (h < a.nq + kv.nkv) {
+    const float* gain = h < a.nq ? a.q_gain : a.k_gain;
+    if (gain != nullptr) {
+      float ss = (lo.x * lo.x + lo.y * lo.y) + (lo.z * lo.z + lo.w * lo.w) + (hi.x * hi.x + hi.y * hi.y) + (hi.z * hi.z + hi.w * hi.w);
+#pragma unroll
+      for (int o = 1; o < LPR; o *= 2) ss += __shfl_xor(ss, o);
+      const float r = 1.0f / sqrtf(ss * (1.0f / DH) + a.eps);
+      const float4 gl = load4(gain + c), gh = load4(gain + DH / 2 + c);
+      lo = make_float4(lo.x * r * gl.x, lo.y * r * gl.y, lo.z * r * gl.z, lo.w * r * gl.w);
+      hi = make_float4(hi.x * r * gh.x, hi.y * r * gh.y, hi.z * r * gh.z, hi.w * r * gh.w);
+    }
+    if (a.rope != nullptr) {
+      const float* t = a.rope + ((size_t)(kv.prefix_len + at.pos) * (DH / 2) + c) * 2;       // (cos, sin) of the four pairs
+      const float4 t0 = load4(t), t1 = load4(t + 4);
+      const float4 u = lo, w = hi;
+      lo = make_float4(u.x * t0.x - w.x * t0.y, u.y * t0.z - w.y * t0.w, u.z * t1.x - w.z * t1.y, u.w * t1.z - w.w * t1.w);
+      hi = make_float4(w.x * t0.x + u.x * t0.y, w.y * t0.z + u.y * t0.w, w.z * t1.x + u.z * t1.y, w.w * t1.z + u.w * t1.w);
+    }
+    if (h < a.nq) {
+      T* q = static_cast<T*>(a.q) + (size_t)i * a.ld_q + (size_t)h * DH;
+      store4(q + c, lo);
+      store4(q + DH / 2 + c, hi);
+    } else if (at.page >= 0) {
+      bf16_t* k = kv.pages + (((size_t)at.page * 2 * kv.nkv + (h - a.nq)) * kv.pt + off) * DH;
+      store4(k + c, lo);
+      store4(k + DH / 2 + c, hi);
+    }
+  } else if (at.page >= 0) {
+    bf16_t* v = kv.pages + ((size_t)at.page * 2 * kv.nkv + (h - a.nq)) * kv.pt * DH + off;
+    const float e[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[(size_t)(c + (j < 4 ? j : DH / 2 + j - 4)) * kv.pt] = f32_to_bf16(e[j]);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// attention
+// ---------------------------------------------------------------------------------------------
+//
+// Row r = (sequence * n_tok + token) * group + query head of a K / V head's rows.  A workgroup takes 32 * WR rows of one K / V head and a
+// range of positions, of the prompt (then the rows are those of all sequences) or of one sequence's own; WT wavefronts share the
+// positions of a tile.  Per 32 positions and 32 rows:
+//   S^T[position][row] = K . Q^T,   O^T[channel][row] += V^T . P^T       (32x32x16 bf16, fp32 accumulators)
+// with a running maximum and sum per row.  K rows are kept in LDS in the order (bits 2 and 3 of the position swapped) that makes a
+// lane's accumulators sixteen positions in two runs of eight: P's operand without a move between lanes.
+// fp32 queries and the probabilities beside them enter as three bf16 terms (24 bits); bf16 queries as they are, and the
+// probabilities rounded to bf16 (2^-9 each, independent: less than the output's own rounding).
+
+struct SoftParts { u32x4 t[3]; };
+
+// Eight floats as bf16 terms.
+template <int TERMS>
+__device__ __forceinline__ SoftParts split_terms(const float (&x)[8]) {
+  SoftParts r;
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = x[i];
+#pragma unroll
+  for (int k = 0; k < TERMS; ++k)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t w = pack_bf16(y[2 * i], y[2 * i + 1]);
+      r.t[k][i] = w;
+      y[2 * i] -= __uint_as_float(w << 16);
+      y[2 * i + 1] -= __uint_as_float(w & 0xffff0000u);
+    }
+  return r;
+}
+
+// Which rows and positions a workgroup takes.
+struct AttnItem {
+  const bf16_t* pool; const int32_t* table; int n_pages;
+  int kvh, row0, rows, part;         // row0: of the K / V head's rows
+  int begin, end;                    // positions
+  int first;                         // own positions: those below it are seen by every token of the call (prompt: end)
+};
+
+template <int DH, int WR, int WT, bool F32>
+struct AttnShape {
+  static constexpr int NW = WR * WT, NT = NW * 64, RT = 32 * WR;
+  static constexpr int TT = WT == 1 ? 64 : 32 * WT;            // positions of a tile
+  static constexpr int CK = DH / 8, S16 = DH / 16, CB = DH / 32, TERMS = F32 ? 3 : 1;
+  static constexpr int KCH = TT * CK, VCH = TT * CK;           // 16-byte chunks
+  static constexpr int OLD = DH + 4;                           // merged rows in LDS
+  static constexpr size_t stage_bytes = (size_t)(KCH + VCH) * 16;
+  static constexpr size_t merge_bytes = WT == 1 ? 0 : (size_t)WT * RT * (OLD + 2) * 4;
+  static constexpr size_t lds = stage_bytes > merge_bytes ? stage_bytes : merge_bytes;
+};
+
+template <int DH, int WR, int WT, bool F32>
+__device__ __forceinline__ void attn_item(const SharedAttnArgs& a, const AttnItem& it, char* lds) {
+  typedef AttnShape<DH, WR, WT, F32> Sh;
+  constexpr int CK = Sh::CK, S16 = Sh::S16, CB = Sh::CB, TT = Sh::TT, NT = Sh::NT;
+  u32x4* ks = reinterpret_cast<u32x4*>(lds);
+  u32x4* vs = ks + Sh::KCH;
+  __shared__ int s_odd;                          // a value that is not finite among V entries that not every token sees
+  const SharedKv& kv = a.kv;
+  const int pt = kv.pt, nkv = kv.nkv, grp = a.nq / nkv, T = a.n_tok;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, wr = w / WT, wt = w % WT, col = lane & 31, hf = lane >> 5;
+  const size_t head_elems = (size_t)pt * DH, page_elems = 2 * (size_t)nkv * head_elems;
+
+  const int r_in = 32 * wr + col, r = it.row0 + min(r_in, it.rows - 1);      // this lane's row (surplus lanes repeat the last)
+  const int tok_row = r / grp, t_own = tok_row % T;
+  bf16x8 q[S16][Sh::TERMS];
+  {
+    const size_t at = (size_t)tok_row * a.ld_q + (size_t)(it.kvh * grp + r % grp) * DH + 8 * hf;
+#pragma unroll
+    for (int s = 0; s < S16; ++s) {
+      if constexpr (F32) {
+        const float* p = static_cast<const float*>(a.q) + at + 16 * s;
+        const float4 x0 = load4(p), x1 = load4(p + 4);
+        const float x[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+        const SoftParts sp = split_terms<Sh::TERMS>(x);
+#pragma unroll
+        for (int k = 0; k < Sh::TERMS; ++k) q[s][k] = as_bf16x8(sp.t[k]);
+      } else {
+        q[s][0] = as_bf16x8(*reinterpret_cast<const u32x4*>(static_cast<const bf16_t*>(a.q) + at + 16 * s));
+      }
+    }
+  }
+  f32x16 O[CB];
+#pragma unroll
+  for (int c = 0; c < CB; ++c)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) O[c][v] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+  const float ce = a.scale * LOG2E;
+  const int see = min(it.end, it.first + t_own);                // positions that this row sees
+  if (tid == 0) s_odd = 0;
+
+  for (int t0 = it.begin; t0 < it.end; t0 += TT) {
+    __syncthreads();
+    for (int i = tid; i < Sh::KCH; i += NT) {                   // K: chunk c of position t0 + p
+      const int p = i / CK, c = i % CK, pos = t0 + p;
+      u32x4 v = {0u, 0u, 0u, 0u};
+      if (pos < it.end) {
+        const int lp = page_of(kv, pos), page = it.table ? it.table[lp] : lp;
+        if ((unsigned)page < (unsigned)it.n_pages)
+          v = *reinterpret_cast<const u32x4*>(it.pool + (size_t)page * page_elems + it.kvh * head_elems + (size_t)(pos - lp * pt) * DH + c * 8);
+        else
+          v = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+      }
+      const int row = (p & ~12) | ((p & 4) << 1) | ((p & 8) >> 1);
+      ks[row * CK + (c ^ (row & (CK - 1)))] = v;
+    }
+    for (int i = tid; i < Sh::VCH; i += NT) {                   // V: eight positions of a channel
+      const int g = i / (2 * DH), ch = (i >> 1) % DH, half = i & 1, pos = t0 + 16 * g + 8 * half;
+      u32x4 v = {0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {                             // (a page may end after the first four)
+        const int pu = pos + 4 * u;
+        if (pu < it.end) {
+          const int lp = page_of(kv, pu), page = it.table ? it.table[lp] : lp;
+          if ((unsigned)page < (unsigned)it.n_pages) {
+            const uint2 x = *reinterpret_cast<const uint2*>(it.pool + (size_t)page * page_elems + (nkv + it.kvh) * head_elems + (size_t)ch * pt + (pu - lp * pt));
+            v[2 * u] = x.x; v[2 * u + 1] = x.y;
+          }
+        }
+      }
+      if (pos + 8 > it.first) {                                 // entries that some row does not see
+        const int n = it.end - pos;                             // entries at or beyond the end may be anything: 0 * NaN would poison the sum
+        bool odd = false;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          v[u] &= n >= 2 * u + 2 ? 0xffffffffu : (n == 2 * u + 1 ? 0xffffu : 0u);
+          odd |= (v[u] & 0x7f80u) == 0x7f80u || (v[u] & 0x7f800000u) == 0x7f800000u;
+        }
+        if (odd && it.first < it.end) s_odd = 1;
+      }
+      vs[(g * 2 + half) * DH + ch] = v;
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int b = wt; b < TT / 32; b += WT) {
+      const int base = t0 + 32 * b;
+      if (base >= it.end) break;
+      f32x16 S;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) S[v] = 0.f;
+      const u32x4* kr = ks + (32 * b + col) * CK;
+#pragma unroll
+      for (int s = 0; s < S16; ++s) {
+        const bf16x8 k = as_bf16x8(kr[(2 * s + hf) ^ (col & (CK - 1))]);
+#pragma unroll
+        for (int u = 0; u < Sh::TERMS; ++u) S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[s][u], S, 0, 0, 0);
+      }
+      // lane half hf holds positions base + 16 (v / 8) + 8 hf + v % 8 of its row
+      if (base + 32 > it.first) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (base + 16 * (v >> 3) + 8 * hf + (v & 7) >= see) S[v] = -INFINITY;
+      }
+      float mx = S[0];
+#pragma unroll
+      for (int v = 1; v < 16; ++v) mx = fmaxf(mx, S[v]);
+      const float m_new = fmaxf(m_run, half_max(mx) * ce);
+      const float m_use = m_new == -INFINITY ? 0.f : m_new;     // a row that sees nothing yet
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
+      float p[16], sum = 0.f;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) { p[v] = __builtin_amdgcn_exp2f(fmaf(S[v], ce, -m_use)); sum += p[v]; }
+      l_run = l_run * alpha + sum;
+      m_run = m_new;
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) O[c][v] *= alpha;
+      const bool odd = base + 32 > it.first && s_odd != 0;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const float px[8] = {p[8 * s], p[8 * s + 1], p[8 * s + 2], p[8 * s + 3], p[8 * s + 4], p[8 * s + 5], p[8 * s + 6], p[8 * s + 7]};
+        const SoftParts sp = split_terms<Sh::TERMS>(px);
+        const u32x4* vr = vs + ((2 * b + s) * 2 + hf) * DH + col;
+        if (!odd) {
+#pragma unroll
+          for (int c = 0; c < CB; ++c) {
+            const bf16x8 v = as_bf16x8(vr[32 * c]);
+#pragma unroll
+            for (int u = 0; u < Sh::TERMS; ++u) O[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, as_bf16x8(sp.t[u]), O[c], 0, 0, 0);
+          }
+        } else {
+          // an infinity or NaN that some tokens do not see: a product per token, with only what it sees, of which its rows keep the result
+#pragma unroll 1
+          for (int t = 0; t < T; ++t) {
+            const int n = it.first + t - (base + 16 * s + 8 * hf);
+#pragma unroll
+            for (int c = 0; c < CB; ++c) {
+              u32x4 v = vr[32 * c];
+#pragma unroll
+              for (int u = 0; u < 4; ++u) v[u] &= n >= 2 * u + 2 ? 0xffffffffu : (n == 2 * u + 1 ? 0xffffu : 0u);
+              f32x16 o = O[c];
+#pragma unroll
+              for (int u = 0; u < Sh::TERMS; ++u) o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v), as_bf16x8(sp.t[u]), o, 0, 0, 0);
+#pragma unroll
+              for (int x = 0; x < 16; ++x) O[c][x] = t == t_own ? o[x] : O[c][x];
+            }
+          }
+        }
+      }
+    }
+  }
+  l_run = half_sum(l_run);
+
+  // results of the row: to the output, or as this range's part
+  const size_t head_rows = (size_t)kv.n_seqs * T * grp;
+  auto put = [&](const int row, const int c, float4 o, const float m, const float l) {
+    const int tr = row / grp, head = it.kvh * grp + row % grp;
+    if (a.plan.parts > 1) {
+      store4(a.part + (((size_t)it.part * nkv + it.kvh) * head_rows + row) * DH + c, o);
+      return;
+    }
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    if constexpr (F32) store4(static_cast<float*>(a.out) + (size_t)tr * a.ld_out + (size_t)head * DH + c, o);
+    else store4(static_cast<bf16_t*>(a.out) + (size_t)tr * a.ld_out + (size_t)head * DH + c, o);
+  };
+  auto put_stat = [&](const int row, const float m, const float l) {
+    if (a.plan.parts > 1) a.ml[((size_t)it.part * nkv + it.kvh) * head_rows + row] = make_float2(m, l);
+    else if (a.lse != nullptr) a.lse[(size_t)(row / grp) * a.nq + it.kvh * grp + row % grp] = l == 0.f ? -INFINITY : (m + __log2f(l)) * LN2;
+  };
+  if constexpr (WT == 1) {
+    if (r_in < it.rows) {
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          put(r, 32 * c + 8 * i + 4 * hf, make_float4(O[c][4 * i], O[c][4 * i + 1], O[c][4 * i + 2], O[c][4 * i + 3]), m_run, l_run);
+      if (hf == 0) put_stat(r, m_run, l_run);
+    }
+  } else {
+    float* sm = reinterpret_cast<float*>(lds);                  // [WT][RT] maxima, sums, then rows
+    float* sl = sm + WT * Sh::RT;
+    float* so = sl + WT * Sh::RT;
+    __syncthreads();
+    if (hf == 0) { sm[wt * Sh::RT + r_in] = m_run; sl[wt * Sh::RT + r_in] = l_run; }
+    __syncthreads();
+    float mm = sm[r_in];
+#pragma unroll
+    for (int u = 1; u < WT; ++u) mm = fmaxf(mm, sm[u * Sh::RT + r_in]);
+    const float f = mm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - mm);
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        store4(so + (size_t)(wt * Sh::RT + r_in) * Sh::OLD + 32 * c + 8 * i + 4 * hf,
+               make_float4(O[c][4 * i] * f, O[c][4 * i + 1] * f, O[c][4 * i + 2] * f, O[c][4 * i + 3] * f));
+    __syncthreads();
+    for (int i = tid; i < it.rows * (DH / 4); i += NT) {
+      const int row = i / (DH / 4), c = i % (DH / 4) * 4;
+      float m = sm[row], l = 0.f;
+#pragma unroll
+      for (int u = 1; u < WT; ++u) m = fmaxf(m, sm[u * Sh::RT + row]);
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int u = 0; u < WT; ++u) {
+        const float4 x = load4(so + (size_t)(u * Sh::RT + row) * Sh::OLD + c);
+        o = make_float4(o.x + x.x, o.y + x.y, o.z + x.z, o.w + x.w);
+        l += m == -INFINITY ? 0.f : sl[u * Sh::RT + row] * __builtin_amdgcn_exp2f(sm[u * Sh::RT + row] - m);
+      }
+      put(it.row0 + row, c, o, m, l);
+      if (c == 0) put_stat(it.row0 + row, m, l);
+    }
+  }
+}
+
+// Workgroups of the prompt's ranges first (n_prefix of them), then those of the own positions.
+template <int DH, int WR, int WT, bool F32>
+__global__ __launch_bounds__(WR * WT * 64) void k_shared_attn(SharedAttnArgs a, int n_prefix) {
+  typedef AttnShape<DH, WR, WT, F32> Sh;
+  __shared__ __align__(16) char lds[Sh::lds];
+  const SharedAttnPlan& p = a.plan;
+  const SharedKv& kv = a.kv;
+  const int grp = a.nq / kv.nkv;
+  AttnItem it;
+  int b = blockIdx.x;
+  if (b < n_prefix) {
+    it.kvh = b % kv.nkv; b /= kv.nkv;
+    const int split = b % p.prefix_splits, tile = b / p.prefix_splits;
+    const int rows = kv.n_seqs * a.n_tok * grp;
+    it.pool = kv.prefix; it.table = kv.prefix_table; it.n_pages = kv.n_prefix_pages;
+    it.row0 = tile * Sh::RT; it.rows = min(Sh::RT, rows - it.row0);
+    it.begin = split * p.prefix_len; it.end = min(kv.prefix_len, it.begin + p.prefix_len); it.first = it.end;
+    it.part = split;
+  } else {
+    b -= n_prefix;
+    it.kvh = b % kv.nkv; b /= kv.nkv;
+    const int split = b % p.own_splits; b /= p.own_splits;
+    const int tile = b % p.own_tiles, seq = b / p.own_tiles;
+    const int rows = a.n_tok * grp, len = min(kv.lens[seq], kv.table_ld * kv.pt);
+    it.pool = kv.pages; it.table = kv.tables + (size_t)seq * kv.table_ld; it.n_pages = kv.n_pages;
+    it.row0 = seq * rows + tile * Sh::RT; it.rows = min(Sh::RT, rows - tile * Sh::RT);
+    it.begin = split * p.own_len; it.end = split + 1 == p.own_splits ? len : min(len, it.begin + p.own_len);
+    it.first = len - a.n_tok + 1;
+    it.part = p.prefix_splits + split;
+  }
+  attn_item<DH, WR, WT, F32>(a, it, lds);
+}
+
+// The parts of a row put together: one wavefront a row.
+template <int DH, bool F32>
+__global__ __launch_bounds__(256) void k_shared_merge(SharedAttnArgs a) {
+  constexpr int LPR = DH / 4, RPW = 256 / LPR;
+  const SharedKv& kv = a.kv;
+  const int grp = a.nq / kv.nkv;
+  const size_t head_rows = (size_t)kv.n_seqs * a.n_tok * grp, total = head_rows * kv.nkv;
+  const size_t i = (size_t)blockIdx.x * RPW + threadIdx.x / LPR;
+  if (i >= total) return;
+  const int c = (threadIdx.x % LPR) * 4;
+  float m = -INFINITY;
+  for (int p = 0; p < a.plan.parts; ++p) m = fmaxf(m, a.ml[p * total + i].x);
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  float l = 0.f;
+  for (int p = 0; p < a.plan.parts; ++p) {
+    const float2 s = a.ml[p * total + i];
+    if (s.y == 0.f) continue;                                   // a range of which the row sees nothing
+    const float f = __builtin_amdgcn_exp2f(s.x - m);
+    const float4 x = load4(a.part + (p * total + i) * DH + c);
+    l += s.y * f;
+    o = make_float4(fmaf(x.x, f, o.x), fmaf(x.y, f, o.y), fmaf(x.z, f, o.z), fmaf(x.w, f, o.w));
+  }
+  const int kvh = (int)(i / head_rows), row = (int)(i % head_rows), tr = row / grp, head = kvh * grp + row % grp;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+  if constexpr (F32) store4(static_cast<float*>(a.out) + (size_t)tr * a.ld_out + (size_t)head * DH + c, o);
+  else store4(static_cast<bf16_t*>(a.out) + (size_t)tr * a.ld_out + (size_t)head * DH + c, o);
+  if (c == 0 && a.lse != nullptr) a.lse[(size_t)tr * a.nq + head] = l == 0.f ? -INFINITY : (m + __log2f(l)) * LN2;
+}
+
+// ---------------------------------------------------------------------------------------------
+// beam selection
+// ---------------------------------------------------------------------------------------------
+//
+// key(b, v) = score_b + x_bv - logsumexp(x_b).  Inside a row the order is that of the logits themselves; between rows the keys are
+// compared in 64 bits.
+
+__device__ __forceinline__ float logit(const float* p) { return *p; }
+__device__ __forceinline__ float logit(const bf16_t* p) { return bf16_to_f32(*p); }
+
+// Order-preserving float -> uint32
+__device__ __forceinline__ uint32_t order_key(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float((k >> 31) ? k ^ 0x80000000u : ~k); }
+
+// The largest of a workgroup's values; every thread gets it.
+__device__ __forceinline__ unsigned long long block_max_u64(unsigned long long v, unsigned long long* sm) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) { const unsigned long long y = __shfl_xor(v, o); v = y > v ? y : v; }
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = sm[0];
+  for (int i = 1; i < (int)(blockDim.x >> 6); ++i) v = sm[i] > v ? sm[i] : v;
+  return v;
+}
+__device__ __forceinline__ float block_sum_f(float v, float* sm) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0.f;
+  for (int i = 0; i < (int)(blockDim.x >> 6); ++i) v += sm[i];
+  return v;
+}
+
+// One chunk of a row: maximum, sum of exponentials, the k largest logits as (order key, ~index), equal logits by the lower index.
+template <typename T>
+__global__ __launch_bounds__(256) void k_beam_chunk(BeamSelectArgs a) {
+  constexpr int E = BEAM_CHUNK / 256;
+  __shared__ unsigned long long sm[4];
+  __shared__ float sf[4];
+  const int chunk = blockIdx.x, row = blockIdx.y, t = threadIdx.x;
+  const T* x = static_cast<const T*>(a.logits) + (size_t)row * a.ld;
+  float v[E], mx = -INFINITY;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int i = chunk * BEAM_CHUNK + e * 256 + t;
+    v[e] = i < a.vocab ? logit(x + i) : -INFINITY;
+    mx = fmaxf(mx, v[e]);
+  }
+  mx = key_value((uint32_t)block_max_u64(order_key(mx), sm));
+  const float m_use = mx == -INFINITY ? 0.f : mx;
+  float sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) sum += expf(v[e] - m_use);
+  sum = block_sum_f(sum, sf);
+  if (t == 0) a.stats[(size_t)row * a.chunks + chunk] = make_float2(mx, sum);
+  unsigned long long last = ~0ull;
+  for (int k = 0; k < a.k; ++k) {
+    unsigned long long best = 0;                                // 0: nothing left
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const unsigned long long key = ((unsigned long long)order_key(v[e]) << 32) | (uint32_t)~(chunk * BEAM_CHUNK + e * 256 + t);
+      if (v[e] > -INFINITY && key < last && key > best) best = key;
+    }
+    best = block_max_u64(best, sm);
+    if (t == 0) a.cand[((size_t)row * a.chunks + chunk) * a.k + k] = best;
+    last = best == 0 ? 0 : best;
+  }
+}
+
+struct BeamCand { double s; uint32_t at; };      // at = beam * vocab + token
+__device__ __forceinline__ bool better(const BeamCand& x, const BeamCand& y) { return x.s > y.s || (x.s == y.s && x.at < y.at); }
+
+__global__ __launch_bounds__(256) void k_beam_merge(BeamSelectArgs a) {
+  __shared__ double s_lse[64];
+  __shared__ double s_s[4];
+  __shared__ uint32_t s_at[4];
+  __shared__ int s_bad;
+  const int g = blockIdx.x, t = threadIdx.x;
+  if (t == 0) s_bad = 0;
+  __syncthreads();
+  for (int b = t; b < a.n_beams; b += 256) {
+    const int row = g * a.n_beams + b;
+    float m = -INFINITY;
+    bool bad = !(a.scores[row] < INFINITY);
+    const bool done = a.done != nullptr && a.done[row] != 0;
+    double sum = 0.0;
+    for (int c = 0; c < a.chunks; ++c) m = fmaxf(m, a.stats[(size_t)row * a.chunks + c].x);
+    for (int c = 0; c < a.chunks; ++c) {
+      const float2 s = a.stats[(size_t)row * a.chunks + c];
+      bad |= !done && !(s.y < INFINITY);
+      if (s.x > -INFINITY) sum += (double)s.y * exp((double)s.x - (double)m);
+    }
+    s_lse[b] = (double)m + log(sum);
+    if (bad) s_bad = 1;
+  }
+  __syncthreads();
+  const int per_row = a.chunks * a.k, n = a.n_beams * per_row;
+  BeamCand last{INFINITY, 0};
+  for (int k = 0; k < a.k; ++k) {
+    BeamCand best{-INFINITY, 0xffffffffu};
+    for (int i = t; i < n; i += 256) {
+      const int b = i / per_row, row = g * a.n_beams + b;
+      BeamCand c;
+      if (a.done != nullptr && a.done[row] != 0) {
+        if (i % per_row != 0) continue;
+        c.s = (double)a.scores[row]; c.at = (uint32_t)(b * a.vocab + a.end_token);
+      } else {
+        const unsigned long long key = a.cand[(size_t)row * per_row + i % per_row];
+        if (key == 0) continue;
+        c.s = (double)a.scores[row] + ((double)key_value((uint32_t)(key >> 32)) - s_lse[b]);
+        c.at = (uint32_t)b * a.vocab + ~(uint32_t)key;
+      }
+      if (c.s > -INFINITY && (k == 0 || better(last, c)) && better(c, best)) best = c;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const BeamCand y{__shfl_xor(best.s, o), (uint32_t)__shfl_xor((int)best.at, o)};
+      if (better(y, best)) best = y;
+    }
+    __syncthreads();
+    if ((t & 63) == 0) { s_s[t >> 6] = best.s; s_at[t >> 6] = best.at; }
+    __syncthreads();
+    for (int i = 0; i < 4; ++i) { const BeamCand y{s_s[i], s_at[i]}; if (better(y, best)) best = y; }
+    if (t == 0) {
+      const size_t o = (size_t)g * a.k + k;
+      const bool none = best.s == -INFINITY || s_bad;
+      const int parent = none ? -1 : (int)(best.at / (uint32_t)a.vocab), token = none ? -1 : (int)(best.at % (uint32_t)a.vocab);
+      a.tokens[o] = token; a.parents[o] = parent;
+      a.scores_out[o] = s_bad ? NAN : (none ? -INFINITY : (float)best.s);
+      if (a.done_out != nullptr)
+        a.done_out[o] = none ? 1 : ((a.done != nullptr && a.done[g * a.n_beams + parent] != 0) || token == a.end_token ? 1 : 0);
+    }
+    last = best;
+    if (best.s == -INFINITY) last.at = 0xffffffffu;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// reordering
+// ---------------------------------------------------------------------------------------------
+
+// Sequence b of a group goes on from sequence parents[b].  Pages that are full are shared by reference; of the one being filled
+// the first child takes its parent's, further children get those of sequences without a child, with the contents copied.
+__global__ __launch_bounds__(256) void k_beam_reorder(BeamReorderArgs a, int copy_wgs) {
+  __shared__ int s_par[64], s_dst[64], s_src[64];
+  const int nb = a.n_beams, t = threadIdx.x;
+  const int unit = blockIdx.x, g = blockIdx.y;
+  const int32_t* old = a.tables + (size_t)g * nb * a.table_ld;
+  if (t < 64) {
+    int p = t < nb ? a.parents[(size_t)g * nb + t] : -1;
+    if (t < nb && (unsigned)p >= (unsigned)nb) p = t;
+    s_par[t] = p;
+    // (one wavefront: every lane sees all parents)
+    bool further = false, childless = t < nb;
+    for (int j = 0; j < nb; ++j) {
+      const int pj = __shfl(p, j);
+      further |= j < t && pj == p;
+      childless &= pj != t;
+    }
+    further &= t < nb;
+    const unsigned long long fm = __ballot(further), em = __ballot(childless);
+    const int rank = __popcll(fm & ((1ull << t) - 1));
+    unsigned long long rest = em;                               // the rank-th sequence without a child
+    for (int j = 0; j < rank; ++j) rest &= rest - 1;
+    const int own = t < nb && a.live ? old[(size_t)(further ? __ffsll(rest) - 1 : p) * a.table_ld + a.full] : 0;
+    s_dst[t] = own;
+    s_src[t] = further && a.live ? old[(size_t)p * a.table_ld + a.full] : -1;
+  }
+  __syncthreads();
+  if (unit < copy_wgs) {                                        // a layer of the pages to be copied
+    bf16_t* pages = a.pages + (size_t)unit * a.layer_stride;
+    for (int b = 0; b < nb; ++b) {
+      const int src = s_src[b], dst = s_dst[b];
+      if ((unsigned)src >= (unsigned)a.n_pages || (unsigned)dst >= (unsigned)a.n_pages) continue;
+      const u32x4* from = reinterpret_cast<const u32x4*>(pages + (size_t)src * a.page_elems);
+      u32x4* to = reinterpret_cast<u32x4*>(pages + (size_t)dst * a.page_elems);
+      for (int64_t i = t; i < a.page_elems / 8; i += 256) to[i] = from[i];
+    }
+  } else {                                                      // the tables
+    for (int i = t; i < nb * a.table_ld; i += 256) {
+      const int b = i / a.table_ld, c = i % a.table_ld;
+      int32_t v;
+      if (c < a.full) v = old[(size_t)s_par[b] * a.table_ld + c];
+      else if (c == a.full && a.live) v = s_dst[b];
+      else v = old[(size_t)b * a.table_ld + c];
+      a.tables_out[((size_t)g * nb + b) * a.table_ld + c] = v;
+    }
+  }
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------------------------
+
+hipError_t launch_append(const AppendArgs& a, bool fp32, hipStream_t s) {
+  const int rpw = 256 / (a.kv.dh / 8);
+  const dim3 grid((unsigned)((a.rows + rpw - 1) / rpw), (unsigned)(a.nq + 2 * a.kv.nkv));
+  if (a.kv.dh == 128) {
+    if (fp32) hipLaunchKernelGGL((k_append<128, float>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_append<128, bf16_t>), grid, dim3(256), 0, s, a);
+  } else {
+    if (fp32) hipLaunchKernelGGL((k_append<64, float>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_append<64, bf16_t>), grid, dim3(256), 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+SharedAttnPlan shared_attn_plan(int n_seqs, int n_tok, int nq, int nkv, int dh, int prefix_len, int max_len) {
+  SharedAttnPlan p{};
+  const long grp = nq / nkv, own_rows = n_tok * grp, rows = n_seqs * own_rows;
+  auto ranges = [](long tiles, int len, int step, int* splits, int* range) {
+    long n = (512 + tiles - 1) / tiles;
+    const long most = (len + 255) / 256;
+    n = n < 1 ? 1 : (n > most ? (most < 1 ? 1 : most) : n);
+    if (n > 64) n = 64;
+    long r = (len + n - 1) / n;
+    r = (r + step - 1) / step * step;
+    if (r < step) r = step;
+    *range = (int)r;
+    *splits = (int)((len + r - 1) / r);
+    if (*splits < 1) *splits = 1;
+  };
+  if (prefix_len > 0) {
+    p.wr_prefix = rows <= 32 ? 1 : (rows <= 64 ? 2 : (rows <= 128 ? 4 : 8));
+    p.prefix_tiles = (int)((rows + 32 * p.wr_prefix - 1) / (32 * p.wr_prefix));
+    ranges((long)p.prefix_tiles * nkv, prefix_len, 256, &p.prefix_splits, &p.prefix_len);
+  }
+  p.wr_own = own_rows <= 32 ? 1 : (own_rows <= 64 ? 2 : (own_rows <= 128 ? 4 : 8));
+  p.own_tiles = (int)((own_rows + 32 * p.wr_own - 1) / (32 * p.wr_own));
+  ranges((long)p.own_tiles * nkv * n_seqs, max_len, 256, &p.own_splits, &p.own_len);
+  p.parts = p.prefix_splits + p.own_splits;
+  if (p.parts > 1) p.bytes = (size_t)p.parts * rows * nkv * (dh * sizeof(float) + sizeof(float2));
+  return p;
+}
+
+template <int DH, bool F32>
+static void launch_attn_wr(int wr, unsigned n, int n_prefix, const SharedAttnArgs& a, hipStream_t s) {
+  switch (wr) {
+    case 1: hipLaunchKernelGGL((k_shared_attn<DH, 1, 4, F32>), dim3(n), dim3(256), 0, s, a, n_prefix); break;
+    case 2: hipLaunchKernelGGL((k_shared_attn<DH, 2, 2, F32>), dim3(n), dim3(256), 0, s, a, n_prefix); break;
+    case 4: hipLaunchKernelGGL((k_shared_attn<DH, 4, 1, F32>), dim3(n), dim3(256), 0, s, a, n_prefix); break;
+    default: hipLaunchKernelGGL((k_shared_attn<DH, 8, 1, F32>), dim3(n), dim3(512), 0, s, a, n_prefix); break;
+  }
+}
+
+template <int DH, bool F32>
+static hipError_t launch_attn_all(const SharedAttnArgs& a, hipStream_t s) {
+  const SharedAttnPlan& p = a.plan;
+  const unsigned n_prefix = (unsigned)(p.prefix_tiles * p.prefix_splits * a.kv.nkv), n_own = (unsigned)(a.kv.n_seqs * p.own_tiles * p.own_splits * a.kv.nkv);
+  if (n_prefix == 0 || p.wr_prefix == p.wr_own) {
+    launch_attn_wr<DH, F32>(p.wr_own, n_prefix + n_own, (int)n_prefix, a, s);
+  } else {
+    launch_attn_wr<DH, F32>(p.wr_prefix, n_prefix, (int)n_prefix, a, s);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    launch_attn_wr<DH, F32>(p.wr_own, n_own, 0, a, s);
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.parts == 1) return e;
+  const size_t rows = (size_t)a.kv.n_seqs * a.n_tok * a.nq;
+  constexpr int rpw = 256 / (DH / 4);
+  hipLaunchKernelGGL((k_shared_merge<DH, F32>), dim3((unsigned)((rows + rpw - 1) / rpw)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_shared_attn(const SharedAttnArgs& a, bool fp32, hipStream_t s) {
+  if (a.kv.dh == 128) return fp32 ? launch_attn_all<128, true>(a, s) : launch_attn_all<128, false>(a, s);
+  return fp32 ? launch_attn_all<64, true>(a, s) : launch_attn_all<64, false>(a, s);
+}
+
+hipError_t launch_beam_select(const BeamSelectArgs& a, bool fp32, hipStream_t s) {
+  const dim3 grid((unsigned)a.chunks, (unsigned)(a.n_groups * a.n_beams));
+  if (fp32) hipLaunchKernelGGL(k_beam_chunk<float>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(k_beam_chunk<bf16_t>, grid, dim3(256), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(k_beam_merge, dim3((unsigned)a.n_groups), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_beam_reorder(const BeamReorderArgs& a, hipStream_t s) {
+  const int copies = a.live ? a.n_layers : 0;
+  hipLaunchKernelGGL(k_beam_reorder, dim3((unsigned)(copies + 1), (unsigned)a.n_groups), dim3(256), 0, s, a, copies);
+  return hipGetLastError();
+}
+
+}  // namespace disco
