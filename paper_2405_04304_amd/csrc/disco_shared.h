@@ -44,14 +44,15 @@ struct SharedAttnArgs {
 };
 hipError_t launch_shared_attn(const SharedAttnArgs& a, bool fp32, hipStream_t s);
 
-constexpr int BEAM_CHUNK = 4096;     // logits of a workgroup
+constexpr int DISCO_BEAM_MAX_ROWS = 64;
+int beam_unit_logits(int rows, int vocab);   // logits of a unit
 struct BeamSelectArgs {
   const void* logits; int64_t ld; int n_groups, n_beams, vocab, k;
   const float* scores; const int32_t* done; int end_token;
   int32_t* tokens; int32_t* parents; float* scores_out; int32_t* done_out;
-  float2* stats;                     // [row][chunk]: maximum, sum of exponentials
-  unsigned long long* cand;          // [row][chunk][k]
-  int chunks;
+  float2* stats;                     // [row][unit]: maximum, sum of exponentials
+  unsigned long long* cand;          // [row][unit][k]: (order key, ~index), descending, 0 behind the last
+  int units;
 };
 hipError_t launch_beam_select(const BeamSelectArgs& a, bool fp32, hipStream_t s);
 

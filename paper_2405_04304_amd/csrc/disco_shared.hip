@@ -428,141 +428,241 @@ __global__ __launch_bounds__(256) void k_shared_merge(SharedAttnArgs a) {
 // ---------------------------------------------------------------------------------------------
 //
 // key(b, v) = score_b + x_bv - logsumexp(x_b).  Inside a row the order is that of the logits themselves; between rows the keys are
-// compared in 64 bits.
+// compared in 64 bits.  Two launches: a wavefront per unit of 64 E logits of a row holds them in registers and leaves their maximum,
+// their sum of exponentials and the k largest in order; a workgroup per group merges the units of each row (a wavefront a row) and
+// ranks the rows' k best against each other.  The k largest of many come from a bound (the k-th largest of 256 partial maxima), a
+// list of what reaches it, and the rank of each entry of the list: no sort and no rounds of k.
 
 __device__ __forceinline__ float logit(const float* p) { return *p; }
 __device__ __forceinline__ float logit(const bf16_t* p) { return bf16_to_f32(*p); }
 
-// Order-preserving float -> uint32
+// Order-preserving float -> uint32 (never 0 for a number or infinity) and back
 __device__ __forceinline__ uint32_t order_key(float x) {
   const uint32_t u = __float_as_uint(x);
-  return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float((k >> 31) ? k ^ 0x80000000u : ~k); }
 
-// The largest of a workgroup's values; every thread gets it.
-__device__ __forceinline__ unsigned long long block_max_u64(unsigned long long v, unsigned long long* sm) {
+__device__ __forceinline__ uint32_t wave_max_key(uint32_t v) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) { const unsigned long long y = __shfl_xor(v, o); v = y > v ? y : v; }
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = sm[0];
-  for (int i = 1; i < (int)(blockDim.x >> 6); ++i) v = sm[i] > v ? sm[i] : v;
-  return v;
+  for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o));
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
 }
-__device__ __forceinline__ float block_sum_f(float v, float* sm) {
+__device__ __forceinline__ float wave_sum_f(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = 0.f;
-  for (int i = 0; i < (int)(blockDim.x >> 6); ++i) v += sm[i];
   return v;
 }
 
-// One chunk of a row: maximum, sum of exponentials, the k largest logits as (order key, ~index), equal logits by the lower index.
-template <typename T>
-__global__ __launch_bounds__(256) void k_beam_chunk(BeamSelectArgs a) {
-  constexpr int E = BEAM_CHUNK / 256;
-  __shared__ unsigned long long sm[4];
-  __shared__ float sf[4];
-  const int chunk = blockIdx.x, row = blockIdx.y, t = threadIdx.x;
-  const T* x = static_cast<const T*>(a.logits) + (size_t)row * a.ld;
-  float v[E], mx = -INFINITY;
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const int i = chunk * BEAM_CHUNK + e * 256 + t;
-    v[e] = i < a.vocab ? logit(x + i) : -INFINITY;
-    mx = fmaxf(mx, v[e]);
+// A bound that at least k of the wavefront's 256 values reach (0 where fewer are not 0): the k-th largest but for its last 12 bits.
+__device__ __forceinline__ uint32_t kth_bound(const uint32_t (&m)[4], const int k) {
+  const uint32_t top = wave_max_key(max(max(m[0], m[1]), max(m[2], m[3])));
+  uint32_t cur = 0;
+  for (int bit = 31; bit >= 12; --bit) {
+    const uint32_t t = cur | (1u << bit);
+    if (t > top) continue;
+    const int n = __popcll(__ballot(m[0] >= t)) + __popcll(__ballot(m[1] >= t)) + __popcll(__ballot(m[2] >= t)) + __popcll(__ballot(m[3] >= t));
+    if (n >= k) cur = t;
   }
-  mx = key_value((uint32_t)block_max_u64(order_key(mx), sm));
-  const float m_use = mx == -INFINITY ? 0.f : mx;
-  float sum = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) sum += expf(v[e] - m_use);
-  sum = block_sum_f(sum, sf);
-  if (t == 0) a.stats[(size_t)row * a.chunks + chunk] = make_float2(mx, sum);
-  unsigned long long last = ~0ull;
-  for (int k = 0; k < a.k; ++k) {
-    unsigned long long best = 0;                                // 0: nothing left
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const unsigned long long key = ((unsigned long long)order_key(v[e]) << 32) | (uint32_t)~(chunk * BEAM_CHUNK + e * 256 + t);
-      if (v[e] > -INFINITY && key < last && key > best) best = key;
+  return cur;
+}
+
+// What the wavefront's lanes have written to LDS is there for all of them (the unit works in order: this only holds the compiler).
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+constexpr int BEAM_LIST = 256;       // keys of a wavefront's list
+
+// The k largest of a wavefront's keys (distinct, 0: none), in order, to out[0 .. k).  visit(f) calls f(key) in every lane for the same number
+// of keys, as many times as asked; bound: at least k keys reach bound << 32 (or all do).
+template <typename Visit>
+__device__ __forceinline__ void wave_top_k(Visit visit, const uint32_t bound, const int k, unsigned long long* list, unsigned long long* out) {
+  const int lane = threadIdx.x & 63;
+  unsigned long long least = (unsigned long long)max(bound, 1u) << 32;
+  int n = 0;
+  auto collect = [&]() {
+    n = 0;
+    visit([&](const unsigned long long key) {
+      const unsigned long long hit = __ballot(key >= least);
+      if (hit == 0) return;
+      if (key >= least) {
+        const int at = n + __popcll(hit & ((1ull << lane) - 1));
+        if (at < BEAM_LIST) list[at] = key;
+      }
+      n += __popcll(hit);
+    });
+  };
+  collect();
+  if (n > BEAM_LIST) {               // many equal values: the k-th largest key itself, bit by bit
+    unsigned long long cur = 0;
+    for (int bit = 63; bit >= 0; --bit) {
+      const unsigned long long t = cur | (1ull << bit);
+      int c = 0;
+      visit([&](const unsigned long long key) { c += __popcll(__ballot(key >= t)); });
+      if (c >= k) cur = t;
     }
-    best = block_max_u64(best, sm);
-    if (t == 0) a.cand[((size_t)row * a.chunks + chunk) * a.k + k] = best;
-    last = best == 0 ? 0 : best;
+    least = cur;
+    collect();
+  }
+  wave_lds_fence();
+  for (int i = lane; i < n; i += 64) {
+    const unsigned long long key = list[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += list[j] > key ? 1 : 0;
+    if (rank < k) out[rank] = key;
+  }
+  for (int i = n + lane; i < k; i += 64) out[i] = 0;
+}
+
+// Eight consecutive logits from index i on, in 16-byte loads wherever the row starts (rows of an odd vocabulary do not start at 16 bytes);
+// -inf beyond the row.
+__device__ __forceinline__ void load_logits(const bf16_t* x, const int i, const int n, float* v) {
+  if (i + 8 <= n) {
+    u32x4 u;
+    __builtin_memcpy(&u, x + i, 16);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { v[2 * e] = __uint_as_float(u[e] << 16); v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u); }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = i + e < n ? bf16_to_f32(x[i + e]) : -INFINITY;
+  }
+}
+__device__ __forceinline__ void load_logits(const float* x, const int i, const int n, float* v) {
+  if (i + 8 <= n) {
+    f32x4 u[2];
+    __builtin_memcpy(u, x + i, 32);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = u[e >> 2][e & 3];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = i + e < n ? x[i + e] : -INFINITY;
   }
 }
 
-struct BeamCand { double s; uint32_t at; };      // at = beam * vocab + token
-__device__ __forceinline__ bool better(const BeamCand& x, const BeamCand& y) { return x.s > y.s || (x.s == y.s && x.at < y.at); }
+template <typename T, int E>
+__global__ __launch_bounds__(256) void k_beam_units(BeamSelectArgs a) {
+  __shared__ unsigned long long lists[4][BEAM_LIST];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int id = blockIdx.x * 4 + w;
+  if (id >= a.n_groups * a.n_beams * a.units) return;
+  const int row = id / a.units, first = (id - row * a.units) * 64 * E;
+  const T* x = static_cast<const T*>(a.logits) + (size_t)row * a.ld;
+  float v[E];
+#pragma unroll
+  for (int e = 0; e < E; e += 8) load_logits(x, first + e * 64 + lane * 8, a.vocab, v + e);
+  // maxima of a quarter of the lane's values each (a NaN stays out of them, and shows in the sum)
+  uint32_t m[4];
+  float mx = -INFINITY;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    float y = v[q * E / 4];
+#pragma unroll
+    for (int e = 1; e < E / 4; ++e) y = fmaxf(y, v[q * E / 4 + e]);
+    y = fmaxf(y, -INFINITY);
+    m[q] = y > -INFINITY ? order_key(y) : 0u;
+    mx = fmaxf(mx, y);
+  }
+  mx = key_value(wave_max_key(order_key(mx)));
+  const float m_use = mx == -INFINITY ? 0.f : mx;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int e = 0; e < E; ++e) sum[e & 3] += __builtin_amdgcn_exp2f((v[e] - m_use) * LOG2E);
+  const float total = wave_sum_f((sum[0] + sum[1]) + (sum[2] + sum[3]));
+  if (lane == 0) a.stats[id] = make_float2(mx, total);
+  wave_top_k([&](auto f) {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      f(v[e] > -INFINITY ? ((unsigned long long)order_key(v[e]) << 32) | (uint32_t)~(first + (e & ~7) * 64 + lane * 8 + (e & 7)) : 0ull);
+  }, kth_bound(m, a.k), a.k, lists[w], a.cand + (size_t)id * a.k);
+}
 
-__global__ __launch_bounds__(256) void k_beam_merge(BeamSelectArgs a) {
-  __shared__ double s_lse[64];
-  __shared__ double s_s[4];
-  __shared__ uint32_t s_at[4];
+struct BeamCand { double s; int token; int pad; };   // of one row; equal keys by the lower token
+
+// LDS: candidates [beam][k], keys [wavefront][k], lists [wavefront][BEAM_LIST].  Workgroup of a wavefront per row, up to sixteen.
+__global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
+  extern __shared__ __align__(16) char smem[];
   __shared__ int s_bad;
-  const int g = blockIdx.x, t = threadIdx.x;
+  __shared__ int s_n[DISCO_BEAM_MAX_ROWS];
+  const int g = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6, nw = blockDim.x >> 6, k = a.k;
+  BeamCand* cand = reinterpret_cast<BeamCand*>(smem);
+  unsigned long long* keys = reinterpret_cast<unsigned long long*>(cand + a.n_beams * k) + w * k;
+  unsigned long long* list = reinterpret_cast<unsigned long long*>(cand + a.n_beams * k) + nw * k + w * BEAM_LIST;
   if (t == 0) s_bad = 0;
   __syncthreads();
-  for (int b = t; b < a.n_beams; b += 256) {
+  for (int b = w; b < a.n_beams; b += nw) {
     const int row = g * a.n_beams + b;
-    float m = -INFINITY;
-    bool bad = !(a.scores[row] < INFINITY);
-    const bool done = a.done != nullptr && a.done[row] != 0;
-    double sum = 0.0;
-    for (int c = 0; c < a.chunks; ++c) m = fmaxf(m, a.stats[(size_t)row * a.chunks + c].x);
-    for (int c = 0; c < a.chunks; ++c) {
-      const float2 s = a.stats[(size_t)row * a.chunks + c];
-      bad |= !done && !(s.y < INFINITY);
-      if (s.x > -INFINITY) sum += (double)s.y * exp((double)s.x - (double)m);
+    const float score = a.scores[row];
+    bool bad = !(score < INFINITY);
+    int n = 0;
+    if (a.done != nullptr && a.done[row] != 0) {
+      n = score > -INFINITY ? 1 : 0;
+      if (lane == 0) cand[b * k] = BeamCand{(double)score, a.end_token, 0};
+    } else {
+      const float2* st = a.stats + (size_t)row * a.units;
+      float m = -INFINITY;
+      for (int c = lane; c < a.units; c += 64) m = fmaxf(m, st[c].x);
+      m = key_value(wave_max_key(order_key(m)));
+      double sum = 0.0;
+      for (int c = lane; c < a.units; c += 64) {
+        const float2 s = st[c];
+        bad |= !(s.y < INFINITY);
+        if (s.x > -INFINITY) sum += (double)s.y * exp((double)s.x - (double)m);
+      }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+      bad = __any(bad);
+      const double off = (double)score - ((double)m + log(sum));
+      if (!bad && score > -INFINITY && m > -INFINITY) {
+        const unsigned long long* src = a.cand + (size_t)row * a.units * k;
+        const int total = a.units * k;
+        uint32_t q[4] = {0u, 0u, 0u, 0u};
+        for (int i = 0; i < total; i += 256)
+#pragma unroll
+          for (int u = 0; u < 4; ++u) { const int j = i + u * 64 + lane; if (j < total) q[u] = max(q[u], (uint32_t)(src[j] >> 32)); }
+        wave_top_k([&](auto f) {
+          for (int i = 0; i < total; i += 64) f(i + lane < total ? src[i + lane] : 0ull);
+        }, kth_bound(q, k), k, list, keys);
+        wave_lds_fence();
+        for (int i = lane; i < k; i += 64) {
+          const unsigned long long key = keys[i];
+          if (key != 0) cand[b * k + i] = BeamCand{off + (double)key_value((uint32_t)(key >> 32)), (int)~(uint32_t)key, 0};
+          n += __popcll(__ballot(key != 0));
+        }
+        n = __builtin_amdgcn_readfirstlane(n);
+      }
     }
-    s_lse[b] = (double)m + log(sum);
-    if (bad) s_bad = 1;
+    if (lane == 0) { s_n[b] = n; if (bad) s_bad = 1; }
   }
   __syncthreads();
-  const int per_row = a.chunks * a.k, n = a.n_beams * per_row;
-  BeamCand last{INFINITY, 0};
-  for (int k = 0; k < a.k; ++k) {
-    BeamCand best{-INFINITY, 0xffffffffu};
-    for (int i = t; i < n; i += 256) {
-      const int b = i / per_row, row = g * a.n_beams + b;
-      BeamCand c;
-      if (a.done != nullptr && a.done[row] != 0) {
-        if (i % per_row != 0) continue;
-        c.s = (double)a.scores[row]; c.at = (uint32_t)(b * a.vocab + a.end_token);
-      } else {
-        const unsigned long long key = a.cand[(size_t)row * per_row + i % per_row];
-        if (key == 0) continue;
-        c.s = (double)a.scores[row] + ((double)key_value((uint32_t)(key >> 32)) - s_lse[b]);
-        c.at = (uint32_t)b * a.vocab + ~(uint32_t)key;
+  const bool bad = s_bad != 0;
+  int have = 0;
+  for (int b = 0; b < a.n_beams; ++b) have += s_n[b];
+  for (int i = t; i < a.n_beams * k; i += blockDim.x) {
+    const int b = i / k, r = i - b * k;
+    if (bad || r >= s_n[b]) continue;
+    const BeamCand c = cand[i];
+    int rank = r;
+    for (int o = 0; o < a.n_beams && rank < k; ++o) {           // better ones of the other rows: their lists are in order
+      if (o == b) continue;
+      int lo = 0, hi = s_n[o];
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        const double y = cand[o * k + mid].s;
+        if (y > c.s || (y == c.s && o < b)) lo = mid + 1; else hi = mid;
       }
-      if (c.s > -INFINITY && (k == 0 || better(last, c)) && better(c, best)) best = c;
+      rank += lo;
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const BeamCand y{__shfl_xor(best.s, o), (uint32_t)__shfl_xor((int)best.at, o)};
-      if (better(y, best)) best = y;
-    }
-    __syncthreads();
-    if ((t & 63) == 0) { s_s[t >> 6] = best.s; s_at[t >> 6] = best.at; }
-    __syncthreads();
-    for (int i = 0; i < 4; ++i) { const BeamCand y{s_s[i], s_at[i]}; if (better(y, best)) best = y; }
-    if (t == 0) {
-      const size_t o = (size_t)g * a.k + k;
-      const bool none = best.s == -INFINITY || s_bad;
-      const int parent = none ? -1 : (int)(best.at / (uint32_t)a.vocab), token = none ? -1 : (int)(best.at % (uint32_t)a.vocab);
-      a.tokens[o] = token; a.parents[o] = parent;
-      a.scores_out[o] = s_bad ? NAN : (none ? -INFINITY : (float)best.s);
-      if (a.done_out != nullptr)
-        a.done_out[o] = none ? 1 : ((a.done != nullptr && a.done[g * a.n_beams + parent] != 0) || token == a.end_token ? 1 : 0);
-    }
-    last = best;
-    if (best.s == -INFINITY) last.at = 0xffffffffu;
+    if (rank >= k) continue;
+    const size_t at = (size_t)g * k + rank;
+    a.tokens[at] = c.token; a.parents[at] = b; a.scores_out[at] = (float)c.s;
+    if (a.done_out != nullptr) a.done_out[at] = (a.done != nullptr && a.done[g * a.n_beams + b] != 0) || c.token == a.end_token ? 1 : 0;
+  }
+  for (int i = (bad ? 0 : have) + t; i < k; i += blockDim.x) {
+    const size_t at = (size_t)g * k + i;
+    a.tokens[at] = -1; a.parents[at] = -1; a.scores_out[at] = bad ? NAN : -INFINITY;
+    if (a.done_out != nullptr) a.done_out[at] = 1;
   }
 }
 
@@ -701,13 +801,23 @@ hipError_t launch_shared_attn(const SharedAttnArgs& a, bool fp32, hipStream_t s)
   return fp32 ? launch_attn_all<64, true>(a, s) : launch_attn_all<64, false>(a, s);
 }
 
+// Logits of a lane: 64 where that leaves every SIMD two wavefronts, else 16.
+int beam_unit_logits(int rows, int vocab) { return 64 * ((long)rows * ((vocab + 4095) / 4096) >= 2048 ? 64 : 16); }
+
 hipError_t launch_beam_select(const BeamSelectArgs& a, bool fp32, hipStream_t s) {
-  const dim3 grid((unsigned)a.chunks, (unsigned)(a.n_groups * a.n_beams));
-  if (fp32) hipLaunchKernelGGL(k_beam_chunk<float>, grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(k_beam_chunk<bf16_t>, grid, dim3(256), 0, s, a);
+  const dim3 grid((unsigned)(((long)a.n_groups * a.n_beams * a.units + 3) / 4));
+  const bool wide = beam_unit_logits(a.n_groups * a.n_beams, a.vocab) == 64 * 64;
+  if (fp32 && wide) hipLaunchKernelGGL((k_beam_units<float, 64>), grid, dim3(256), 0, s, a);
+  else if (fp32) hipLaunchKernelGGL((k_beam_units<float, 16>), grid, dim3(256), 0, s, a);
+  else if (wide) hipLaunchKernelGGL((k_beam_units<bf16_t, 64>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_beam_units<bf16_t, 16>), grid, dim3(256), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_beam_merge, dim3((unsigned)a.n_groups), dim3(256), 0, s, a);
+  int nw = a.n_beams < 16 ? a.n_beams : 16;
+  auto lds_bytes = [&]() { return sizeof(BeamCand) * a.n_beams * a.k + sizeof(unsigned long long) * nw * (a.k + BEAM_LIST); };
+  while (nw > 4 && lds_bytes() > (size_t)150 << 10) nw /= 2;    // 64 beams of 128: 128 KiB for the candidates
+  const size_t lds = lds_bytes();
+  hipLaunchKernelGGL(k_beam_merge, dim3((unsigned)a.n_groups), dim3(64 * nw), lds, s, a);
   return hipGetLastError();
 }
 

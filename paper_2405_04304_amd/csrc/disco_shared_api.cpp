@@ -166,11 +166,11 @@ static int check_beams(int n_groups, int n_beams, int vocab, int k) {
   return DISCO_OK;
 }
 
-static int beam_chunks(int vocab) { return (vocab + BEAM_CHUNK - 1) / BEAM_CHUNK; }
+static int beam_units(int rows, int vocab) { const int n = beam_unit_logits(rows, vocab); return (vocab + n - 1) / n; }
 
 size_t disco_beam_select_bytes(int n_groups, int n_beams, int vocab, int k) {
   if (check_beams(n_groups, n_beams, vocab, k)) return 0;
-  const size_t rows = (size_t)n_groups * n_beams, per_row = (size_t)beam_chunks(vocab);
+  const size_t rows = (size_t)n_groups * n_beams, per_row = (size_t)beam_units((int)rows, vocab);
   return round_up(rows * per_row * (8 + 8 * (size_t)k) + 256, 256);
 }
 
@@ -188,12 +188,12 @@ int disco_beam_select(const void* dev_logits, int dtype, int64_t ld_logits, int 
   if (!aligned(dev_logits, dtype == DISCO_F32 ? 4 : 2) || !aligned(dev_scores, 4) || !aligned(dev_done, 4) || !aligned(dev_tokens, 4) || !aligned(dev_parents, 4) ||
       !aligned(dev_scores_out, 4) || !aligned(dev_done_out, 4) || !aligned(dev_ws, 256))
     return fail(DISCO_EINVAL, "misaligned pointer");
-  const size_t need = disco_beam_select_bytes(n_groups, n_beams, vocab, k), rows = (size_t)n_groups * n_beams, per_row = (size_t)beam_chunks(vocab);
+  const size_t need = disco_beam_select_bytes(n_groups, n_beams, vocab, k), rows = (size_t)n_groups * n_beams, per_row = (size_t)beam_units((int)rows, vocab);
   if (ws_bytes < need) return fail(DISCO_EINVAL, "workspace of %zu bytes, %zu needed", ws_bytes, need);
   BeamSelectArgs a{};
   a.logits = dev_logits; a.ld = ld_logits; a.n_groups = n_groups; a.n_beams = n_beams; a.vocab = vocab; a.k = k; a.scores = dev_scores; a.done = dev_done;
   a.end_token = end_token; a.tokens = dev_tokens; a.parents = dev_parents; a.scores_out = dev_scores_out; a.done_out = dev_done_out;
-  a.cand = static_cast<unsigned long long*>(dev_ws); a.stats = reinterpret_cast<float2*>(a.cand + rows * per_row * k); a.chunks = (int)per_row;
+  a.cand = static_cast<unsigned long long*>(dev_ws); a.stats = reinterpret_cast<float2*>(a.cand + rows * per_row * k); a.units = (int)per_row;
   HIP_TRY(launch_beam_select(a, dtype == DISCO_F32, static_cast<hipStream_t>(s)), "beam selection launch");
   return DISCO_OK;
 }

@@ -293,7 +293,7 @@ def _check_select(got, want):
 
 
 SELECT = [(1, 1, 1, 1), (1, 1, 7, 3), (1, 4, 5, 20), (2, 3, 100, 7), (1, 4, 32000, 4), (3, 8, 4096, 16), (2, 5, 4097, 10), (5, 2, 49153, 4), (1, 64, 1000, 64),
-          (1, 2, 131072, 128), (2, 16, 33333, 16)]
+          (1, 2, 131072, 128), (2, 16, 33333, 16), (1, 64, 300, 128), (33, 5, 60000, 12), (1, 1, 1048576, 128)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["fp32", "bf16"])
