@@ -31,6 +31,71 @@ __device__ __forceinline__ HiLo split_bf16(float a, float b) {
   return r;
 }
 
+// Wavefront reductions on the DPP cross-lane network (no LDS traffic): xor-1, xor-2 inside quads,
+// half-row mirror, row mirror, then row broadcasts 15 and 31; lane 63 ends up with the result, which
+// is broadcast through a scalar register.  The combination order is fixed, so sums are reproducible.
+#define DPP_QUAD_XOR1 0xB1
+#define DPP_QUAD_XOR2 0x4E
+#define DPP_ROW_HALF_MIRROR 0x141
+#define DPP_ROW_MIRROR 0x140
+#define DPP_ROW_ROR8 0x128
+#define DPP_ROW_BCAST15 0x142
+#define DPP_ROW_BCAST31 0x143
+
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ float dpp_f(float old, float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(old), __float_as_int(v), CTRL, ROW_MASK, 0xF, false));
+}
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ int dpp_i(int old, int v) {
+  return __builtin_amdgcn_update_dpp(old, v, CTRL, ROW_MASK, 0xF, false);
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+  v += dpp_f<DPP_QUAD_XOR1, 0xF>(0.f, v);
+  v += dpp_f<DPP_QUAD_XOR2, 0xF>(0.f, v);
+  v += dpp_f<DPP_ROW_HALF_MIRROR, 0xF>(0.f, v);
+  v += dpp_f<DPP_ROW_MIRROR, 0xF>(0.f, v);
+  v += dpp_f<DPP_ROW_BCAST15, 0xA>(0.f, v);
+  v += dpp_f<DPP_ROW_BCAST31, 0xC>(0.f, v);
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+__device__ __forceinline__ float wave_max(float v) {
+  v = fmaxf(v, dpp_f<DPP_QUAD_XOR1, 0xF>(v, v));
+  v = fmaxf(v, dpp_f<DPP_QUAD_XOR2, 0xF>(v, v));
+  v = fmaxf(v, dpp_f<DPP_ROW_HALF_MIRROR, 0xF>(v, v));
+  v = fmaxf(v, dpp_f<DPP_ROW_MIRROR, 0xF>(v, v));
+  v = fmaxf(v, dpp_f<DPP_ROW_BCAST15, 0xA>(v, v));
+  v = fmaxf(v, dpp_f<DPP_ROW_BCAST31, 0xC>(v, v));
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// Order-preserving map float -> uint32 (larger float <=> larger key; -inf maps above key 0, which marks
+// a dropped slot) and back.
+__device__ __forceinline__ uint32_t f32_key(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+__device__ __forceinline__ float key_f32(uint32_t k) {
+  return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k);
+}
+// Wavefront maximum of unsigned keys: the cross-lane moves fold into the max instructions (one DPP
+// instruction per step; 0 is the identity, so lanes a step does not reach keep their value).
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ uint32_t dpp_max_u32(uint32_t v) {
+  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROW_MASK, 0xF, true);
+  return v > o ? v : o;
+}
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  v = dpp_max_u32<DPP_QUAD_XOR1, 0xF>(v);
+  v = dpp_max_u32<DPP_QUAD_XOR2, 0xF>(v);
+  v = dpp_max_u32<DPP_ROW_HALF_MIRROR, 0xF>(v);
+  v = dpp_max_u32<DPP_ROW_MIRROR, 0xF>(v);
+  v = dpp_max_u32<DPP_ROW_BCAST15, 0xA>(v);
+  v = dpp_max_u32<DPP_ROW_BCAST31, 0xC>(v);
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+
 // A value and its partner 16 or 32 lanes away, one half of the wavefront each way round (vector instructions; a shuffle goes through
 // the LDS unit).  Lanes that are 16 and 32 apart must be active together.
 struct Pair32 { float a, b; };

@@ -109,45 +109,6 @@ __device__ __forceinline__ HiLo split_product(float a, float ga, float b, float 
   return r;
 }
 
-// Wavefront reductions on the DPP cross-lane network (no LDS traffic): xor-1, xor-2 inside quads,
-// half-row mirror, row mirror, then row broadcasts 15 and 31; lane 63 ends up with the result, which
-// is broadcast through a scalar register.  The combination order is fixed, so sums are reproducible.
-#define DPP_QUAD_XOR1 0xB1
-#define DPP_QUAD_XOR2 0x4E
-#define DPP_ROW_HALF_MIRROR 0x141
-#define DPP_ROW_MIRROR 0x140
-#define DPP_ROW_ROR8 0x128
-#define DPP_ROW_BCAST15 0x142
-#define DPP_ROW_BCAST31 0x143
-
-template <int CTRL, int ROW_MASK>
-__device__ __forceinline__ float dpp_f(float old, float v) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(old), __float_as_int(v), CTRL, ROW_MASK, 0xF, false));
-}
-template <int CTRL, int ROW_MASK>
-__device__ __forceinline__ int dpp_i(int old, int v) {
-  return __builtin_amdgcn_update_dpp(old, v, CTRL, ROW_MASK, 0xF, false);
-}
-
-__device__ __forceinline__ float wave_sum(float v) {
-  v += dpp_f<DPP_QUAD_XOR1, 0xF>(0.f, v);
-  v += dpp_f<DPP_QUAD_XOR2, 0xF>(0.f, v);
-  v += dpp_f<DPP_ROW_HALF_MIRROR, 0xF>(0.f, v);
-  v += dpp_f<DPP_ROW_MIRROR, 0xF>(0.f, v);
-  v += dpp_f<DPP_ROW_BCAST15, 0xA>(0.f, v);
-  v += dpp_f<DPP_ROW_BCAST31, 0xC>(0.f, v);
-  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
-}
-__device__ __forceinline__ float wave_max(float v) {
-  v = fmaxf(v, dpp_f<DPP_QUAD_XOR1, 0xF>(v, v));
-  v = fmaxf(v, dpp_f<DPP_QUAD_XOR2, 0xF>(v, v));
-  v = fmaxf(v, dpp_f<DPP_ROW_HALF_MIRROR, 0xF>(v, v));
-  v = fmaxf(v, dpp_f<DPP_ROW_MIRROR, 0xF>(v, v));
-  v = fmaxf(v, dpp_f<DPP_ROW_BCAST15, 0xA>(v, v));
-  v = fmaxf(v, dpp_f<DPP_ROW_BCAST31, 0xC>(v, v));
-  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
-}
-
 // Hand-off between workgroups of one launch (split reductions).  Data written by one workgroup and
 // read by another inside the same kernel moves with agent-scope relaxed atomic stores / loads: on
 // gfx950 these are write-through / L2-bypassing accesses (sc1), coherent across the eight XCDs'
@@ -1783,32 +1744,6 @@ constexpr int CM_NT = 512;     // threads per slice inside the persistent draft 
 constexpr int CM_SLICE = 1024;     // logits of a workgroup of the many-workgroup launch (32 of them at vocab 32000, 64 at most)
 constexpr int CM_MULTI_NT = 256;   // its threads
 constexpr int CM_REC = 16;     // floats per record
-
-// Order-preserving map float -> uint32 (larger float <=> larger key; -inf maps above key 0, which marks
-// a dropped slot) and back.
-__device__ __forceinline__ uint32_t f32_key(float x) {
-  const uint32_t u = __float_as_uint(x);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
-__device__ __forceinline__ float key_f32(uint32_t k) {
-  return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k);
-}
-// Wavefront maximum of unsigned keys: the cross-lane moves fold into the max instructions (one DPP
-// instruction per step; 0 is the identity, so lanes a step does not reach keep their value).
-template <int CTRL, int ROW_MASK>
-__device__ __forceinline__ uint32_t dpp_max_u32(uint32_t v) {
-  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROW_MASK, 0xF, true);
-  return v > o ? v : o;
-}
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
-  v = dpp_max_u32<DPP_QUAD_XOR1, 0xF>(v);
-  v = dpp_max_u32<DPP_QUAD_XOR2, 0xF>(v);
-  v = dpp_max_u32<DPP_ROW_HALF_MIRROR, 0xF>(v);
-  v = dpp_max_u32<DPP_ROW_MIRROR, 0xF>(v);
-  v = dpp_max_u32<DPP_ROW_BCAST15, 0xA>(v);
-  v = dpp_max_u32<DPP_ROW_BCAST31, 0xC>(v);
-  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
-}
 
 // The ten largest of the N values per lane held by one wavefront, descending, written by lane 0 to
 // out10: ten rounds of a cross-lane maximum over order-preserving integer keys; the first lane that

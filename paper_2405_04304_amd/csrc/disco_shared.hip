@@ -436,27 +436,9 @@ __global__ __launch_bounds__(256) void k_shared_merge(SharedAttnArgs a) {
 __device__ __forceinline__ float logit(const float* p) { return *p; }
 __device__ __forceinline__ float logit(const bf16_t* p) { return bf16_to_f32(*p); }
 
-// Order-preserving float -> uint32 (never 0 for a number or infinity) and back
-__device__ __forceinline__ uint32_t order_key(float x) {
-  const uint32_t u = __float_as_uint(x);
-  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
-}
-__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float((k >> 31) ? k ^ 0x80000000u : ~k); }
-
-__device__ __forceinline__ uint32_t wave_max_key(uint32_t v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o));
-  return (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
-}
-__device__ __forceinline__ float wave_sum_f(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  return v;
-}
-
 // A bound that at least k of the wavefront's 256 values reach (0 where fewer are not 0): the k-th largest but for its last 12 bits.
 __device__ __forceinline__ uint32_t kth_bound(const uint32_t (&m)[4], const int k) {
-  const uint32_t top = wave_max_key(max(max(m[0], m[1]), max(m[2], m[3])));
+  const uint32_t top = wave_max_u32(max(max(m[0], m[1]), max(m[2], m[3])));
   uint32_t cur = 0;
   for (int bit = 31; bit >= 12; --bit) {
     const uint32_t t = cur | (1u << bit);
@@ -475,36 +457,42 @@ __device__ __forceinline__ void wave_lds_fence() {
 
 constexpr int BEAM_LIST = 256;       // keys of a wavefront's list
 
-// The k largest of a wavefront's keys (distinct, 0: none), in order, to out[0 .. k).  visit(f) calls f(key) in every lane for the same number
-// of keys, as many times as asked; bound: at least k keys reach bound << 32 (or all do).
-template <typename Visit>
-__device__ __forceinline__ void wave_top_k(Visit visit, const uint32_t bound, const int k, unsigned long long* list, unsigned long long* out) {
+// The k largest keys of a wavefront that holds n_e a lane, in order, to out[0 .. k) (0 behind the last).  key(e): the e-th, distinct, 0 for none;
+// reaches(e): whether it is one and its value reaches a bound that at least k values reach, or all do.  Every lane calls them for the same e.
+template <int UNROLL, typename Reaches, typename Key>
+__device__ __forceinline__ void wave_top_k(const int n_e, Reaches reaches, Key key, const int k, unsigned long long* list, unsigned long long* out) {
   const int lane = threadIdx.x & 63;
-  unsigned long long least = (unsigned long long)max(bound, 1u) << 32;
   int n = 0;
-  auto collect = [&]() {
-    n = 0;
-    visit([&](const unsigned long long key) {
-      const unsigned long long hit = __ballot(key >= least);
-      if (hit == 0) return;
-      if (key >= least) {
-        const int at = n + __popcll(hit & ((1ull << lane) - 1));
-        if (at < BEAM_LIST) list[at] = key;
-      }
-      n += __popcll(hit);
-    });
+  auto append = [&](const unsigned long long hit, const bool mine, const unsigned long long x) {
+    if (mine) {
+      const int at = n + __popcll(hit & ((1ull << lane) - 1));
+      if (at < BEAM_LIST) list[at] = x;
+    }
+    n += __popcll(hit);
   };
-  collect();
+#pragma unroll UNROLL
+  for (int e = 0; e < n_e; ++e) {
+    const bool mine = reaches(e);
+    const unsigned long long hit = __ballot(mine);
+    if (hit != 0) append(hit, mine, key(e));
+  }
   if (n > BEAM_LIST) {               // many equal values: the k-th largest key itself, bit by bit
     unsigned long long cur = 0;
     for (int bit = 63; bit >= 0; --bit) {
       const unsigned long long t = cur | (1ull << bit);
       int c = 0;
-      visit([&](const unsigned long long key) { c += __popcll(__ballot(key >= t)); });
+#pragma unroll UNROLL
+      for (int e = 0; e < n_e; ++e) c += __popcll(__ballot(key(e) >= t));
       if (c >= k) cur = t;
     }
-    least = cur;
-    collect();
+    n = 0;
+#pragma unroll UNROLL
+    for (int e = 0; e < n_e; ++e) {
+      const unsigned long long x = key(e);
+      const bool mine = x >= cur && x != 0;
+      const unsigned long long hit = __ballot(mine);
+      if (hit != 0) append(hit, mine, x);
+    }
   }
   wave_lds_fence();
   for (int i = lane; i < n; i += 64) {
@@ -561,24 +549,25 @@ __global__ __launch_bounds__(256) void k_beam_units(BeamSelectArgs a) {
 #pragma unroll
     for (int e = 1; e < E / 4; ++e) y = fmaxf(y, v[q * E / 4 + e]);
     y = fmaxf(y, -INFINITY);
-    m[q] = y > -INFINITY ? order_key(y) : 0u;
+    m[q] = y > -INFINITY ? f32_key(y + 0.f) : 0u;
     mx = fmaxf(mx, y);
   }
-  mx = key_value(wave_max_key(order_key(mx)));
+  mx = key_f32(wave_max_u32(f32_key(mx)));
   const float m_use = mx == -INFINITY ? 0.f : mx;
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int e = 0; e < E; ++e) sum[e & 3] += __builtin_amdgcn_exp2f((v[e] - m_use) * LOG2E);
-  const float total = wave_sum_f((sum[0] + sum[1]) + (sum[2] + sum[3]));
+  const float total = wave_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
   if (lane == 0) a.stats[id] = make_float2(mx, total);
-  wave_top_k([&](auto f) {
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-      f(v[e] > -INFINITY ? ((unsigned long long)order_key(v[e]) << 32) | (uint32_t)~(first + (e & ~7) * 64 + lane * 8 + (e & 7)) : 0ull);
-  }, kth_bound(m, a.k), a.k, lists[w], a.cand + (size_t)id * a.k);
+  const uint32_t bound = kth_bound(m, a.k);
+  const float least = bound == 0 ? -3.402823466e38f : key_f32(bound);      // (compared as numbers: a NaN reaches nothing)
+  // + 0: zeros of both signs are equal
+  wave_top_k<E>(E, [&](int e) { return v[e] >= least; }, [&](int e) {
+    return v[e] > -INFINITY ? ((unsigned long long)f32_key(v[e] + 0.f) << 32) | (uint32_t)~(first + (e & ~7) * 64 + lane * 8 + (e & 7)) : 0ull;
+  }, a.k, lists[w], a.cand + (size_t)id * a.k);
 }
 
-struct BeamCand { double s; int token; int pad; };   // of one row; equal keys by the lower token
+struct BeamCand { double s; int token; int rank; };   // of one row; equal keys by the lower token
 
 // LDS: candidates [beam][k], keys [wavefront][k], lists [wavefront][BEAM_LIST].  Workgroup of a wavefront per row, up to sixteen.
 __global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
@@ -603,7 +592,7 @@ __global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
       const float2* st = a.stats + (size_t)row * a.units;
       float m = -INFINITY;
       for (int c = lane; c < a.units; c += 64) m = fmaxf(m, st[c].x);
-      m = key_value(wave_max_key(order_key(m)));
+      m = key_f32(wave_max_u32(f32_key(m)));
       double sum = 0.0;
       for (int c = lane; c < a.units; c += 64) {
         const float2 s = st[c];
@@ -618,16 +607,28 @@ __global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
         const unsigned long long* src = a.cand + (size_t)row * a.units * k;
         const int total = a.units * k;
         uint32_t q[4] = {0u, 0u, 0u, 0u};
-        for (int i = 0; i < total; i += 256)
+        if (total <= 64 * 16) {                                 // in registers, all on their way at once
+          unsigned long long r[16];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) { const int j = i + u * 64 + lane; if (j < total) q[u] = max(q[u], (uint32_t)(src[j] >> 32)); }
-        wave_top_k([&](auto f) {
-          for (int i = 0; i < total; i += 64) f(i + lane < total ? src[i + lane] : 0ull);
-        }, kth_bound(q, k), k, list, keys);
+          for (int e = 0; e < 16; ++e) {
+            r[e] = e * 64 + lane < total ? src[e * 64 + lane] : 0ull;
+            q[e & 3] = max(q[e & 3], (uint32_t)(r[e] >> 32));
+          }
+          const uint32_t least = max(kth_bound(q, k), 1u);
+          wave_top_k<16>(16, [&](int e) { return (uint32_t)(r[e] >> 32) >= least; }, [&](int e) { return r[e]; }, k, list, keys);
+        } else {
+          auto at = [&](int e) { return e * 64 + lane < total ? src[e * 64 + lane] : 0ull; };
+          const int n_e = (total + 63) / 64;
+          for (int e = 0; e < n_e; e += 4)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) q[u] = max(q[u], (uint32_t)(at(e + u) >> 32));
+          const uint32_t least = max(kth_bound(q, k), 1u);
+          wave_top_k<1>(n_e, [&](int e) { return (uint32_t)(at(e) >> 32) >= least; }, at, k, list, keys);
+        }
         wave_lds_fence();
         for (int i = lane; i < k; i += 64) {
           const unsigned long long key = keys[i];
-          if (key != 0) cand[b * k + i] = BeamCand{off + (double)key_value((uint32_t)(key >> 32)), (int)~(uint32_t)key, 0};
+          if (key != 0) cand[b * k + i] = BeamCand{off + (double)key_f32((uint32_t)(key >> 32)), (int)~(uint32_t)key, 0};
           n += __popcll(__ballot(key != 0));
         }
         n = __builtin_amdgcn_readfirstlane(n);
@@ -639,23 +640,29 @@ __global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
   const bool bad = s_bad != 0;
   int have = 0;
   for (int b = 0; b < a.n_beams; ++b) have += s_n[b];
-  for (int i = t; i < a.n_beams * k; i += blockDim.x) {
-    const int b = i / k, r = i - b * k;
-    if (bad || r >= s_n[b]) continue;
-    const BeamCand c = cand[i];
-    int rank = r;
-    for (int o = 0; o < a.n_beams && rank < k; ++o) {           // better ones of the other rows: their lists are in order
-      if (o == b) continue;
+  // rank of every candidate: its place in its own row's list and, counted row by row, the better ones of the others (lists in order)
+  const int n_all = a.n_beams * k;
+  for (int i = t; i < n_all; i += blockDim.x) cand[i].rank = i % k;
+  __syncthreads();
+  if (!bad)
+    for (int i = t; i < n_all * a.n_beams; i += blockDim.x) {
+      const int c = i % n_all, o = i / n_all, b = c / k;
+      if (o == b || c - b * k >= s_n[b]) continue;
+      const double mine = cand[c].s;
       int lo = 0, hi = s_n[o];
       while (lo < hi) {
         const int mid = (lo + hi) >> 1;
         const double y = cand[o * k + mid].s;
-        if (y > c.s || (y == c.s && o < b)) lo = mid + 1; else hi = mid;
+        if (y > mine || (y == mine && o < b)) lo = mid + 1; else hi = mid;
       }
-      rank += lo;
+      if (lo > 0) atomicAdd(&cand[c].rank, lo);
     }
-    if (rank >= k) continue;
-    const size_t at = (size_t)g * k + rank;
+  __syncthreads();
+  for (int i = t; i < n_all; i += blockDim.x) {
+    const int b = i / k;
+    const BeamCand c = cand[i];
+    if (bad || i - b * k >= s_n[b] || c.rank >= k) continue;
+    const size_t at = (size_t)g * k + c.rank;
     a.tokens[at] = c.token; a.parents[at] = b; a.scores_out[at] = (float)c.s;
     if (a.done_out != nullptr) a.done_out[at] = (a.done != nullptr && a.done[g * a.n_beams + b] != 0) || c.token == a.end_token ? 1 : 0;
   }

@@ -311,6 +311,10 @@ def test_select_equal_candidates():
     logits, scores = torch.zeros(6, 5000), torch.tensor([-1.0, -1.0, -2.0, -3.0, -1.0, -1.0])
     logits[:, 4990:] = 1.0
     _check_select(_select(logits, scores, 2, 3, 40), R.select(logits, scores, 2, 3, 40))
+    logits[:, 100:200], logits[:, 150:160] = 2.0, 2.0
+    logits[1, 4000:] = 3.0 * torch.tensor([1.0, -0.0]).repeat(500)       # zeros of both signs are equal
+    logits[0], logits[0, ::3] = 0.0, -0.0
+    _check_select(_select(logits, scores, 2, 3, 100), R.select(logits, scores, 2, 3, 100))
     logits, scores = torch.full((2, 9000), 0.25), torch.zeros(2)
     _check_select(_select(logits, scores, 1, 2, 64), R.select(logits, scores, 1, 2, 64))
 
