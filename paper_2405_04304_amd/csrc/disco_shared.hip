@@ -457,51 +457,56 @@ __device__ __forceinline__ void wave_lds_fence() {
 
 constexpr int BEAM_LIST = 256;       // keys of a wavefront's list
 
-// The k largest keys of a wavefront that holds n_e a lane, in order, to out[0 .. k) (0 behind the last).  key(e): the e-th, distinct, 0 for none;
-// reaches(e): whether it is one and its value reaches a bound that at least k values reach, or all do.  Every lane calls them for the same e.
-template <int UNROLL, typename Reaches, typename Key>
-__device__ __forceinline__ void wave_top_k(const int n_e, Reaches reaches, Key key, const int k, unsigned long long* list, unsigned long long* out) {
+// The k largest keys of a wavefront, in order, to out[0 .. k) (0 behind the last).  visit(f): f(whether the lane's e-th entry reaches the bound,
+// entry) for every e; narrow(): makes the bound the k-th largest key itself; key(entry): distinct.  At least k entries reach the bound, or all do.
+template <typename Visit, typename Narrow, typename Key>
+__device__ __forceinline__ void wave_top_k(Visit visit, Narrow narrow, Key key, const int k, unsigned long long* list, unsigned long long* out) {
   const int lane = threadIdx.x & 63;
   int n = 0;
-  auto append = [&](const unsigned long long hit, const bool mine, const unsigned long long x) {
+  auto append = [&](const bool mine, auto entry) {
+    const unsigned long long hit = __ballot(mine);
+    if (hit == 0) return;
     if (mine) {
-      const int at = n + __popcll(hit & ((1ull << lane) - 1));
-      if (at < BEAM_LIST) list[at] = x;
+      const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hit, 0));
+      if (at < BEAM_LIST) list[at] = entry();
     }
     n += __popcll(hit);
   };
-#pragma unroll UNROLL
-  for (int e = 0; e < n_e; ++e) {
-    const bool mine = reaches(e);
-    const unsigned long long hit = __ballot(mine);
-    if (hit != 0) append(hit, mine, key(e));
-  }
-  if (n > BEAM_LIST) {               // many equal values: the k-th largest key itself, bit by bit
-    unsigned long long cur = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-      const unsigned long long t = cur | (1ull << bit);
-      int c = 0;
-#pragma unroll UNROLL
-      for (int e = 0; e < n_e; ++e) c += __popcll(__ballot(key(e) >= t));
-      if (c >= k) cur = t;
-    }
+  visit(append);
+  if (n > BEAM_LIST) {               // many equal values
+    narrow();
     n = 0;
-#pragma unroll UNROLL
-    for (int e = 0; e < n_e; ++e) {
-      const unsigned long long x = key(e);
-      const bool mine = x >= cur && x != 0;
-      const unsigned long long hit = __ballot(mine);
-      if (hit != 0) append(hit, mine, x);
-    }
+    visit(append);
   }
   wave_lds_fence();
+  for (int i = lane; i < n; i += 64) list[i] = key(list[i]);
+  wave_lds_fence();
   for (int i = lane; i < n; i += 64) {
-    const unsigned long long key = list[i];
+    const unsigned long long mine = list[i];
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += list[j] > key ? 1 : 0;
-    if (rank < k) out[rank] = key;
+    for (int j = 0; j < n; ++j) rank += list[j] > mine ? 1 : 0;
+    if (rank < k) out[rank] = mine;
   }
   for (int i = n + lane; i < k; i += 64) out[i] = 0;
+}
+// The same over keys at(e), n_e a lane.
+template <int UNROLL, typename At>
+__device__ __forceinline__ void wave_top_k_keys(const int n_e, At at, const uint32_t bound, const int k, unsigned long long* list, unsigned long long* out) {
+  unsigned long long least = (unsigned long long)max(bound, 1u) << 32;
+  wave_top_k([&](auto f) {
+#pragma unroll UNROLL
+    for (int e = 0; e < n_e; ++e) { const unsigned long long x = at(e); f(x >= least, [&]() { return x; }); }
+  }, [&]() {
+    least = 0;
+    for (int bit = 63; bit >= 0; --bit) {
+      const unsigned long long t = least | (1ull << bit);
+      int c = 0;
+#pragma unroll UNROLL
+      for (int e = 0; e < n_e; ++e) c += __popcll(__ballot(at(e) >= t));
+      if (c >= k) least = t;
+    }
+    if (least == 0) least = 1;
+  }, [](unsigned long long x) { return x; }, k, list, out);
 }
 
 // Eight consecutive logits from index i on, in 16-byte loads wherever the row starts (rows of an odd vocabulary do not start at 16 bytes);
@@ -559,11 +564,46 @@ __global__ __launch_bounds__(256) void k_beam_units(BeamSelectArgs a) {
   for (int e = 0; e < E; ++e) sum[e & 3] += __builtin_amdgcn_exp2f((v[e] - m_use) * LOG2E);
   const float total = wave_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
   if (lane == 0) a.stats[id] = make_float2(mx, total);
+  // entries: logits of at least `least` (compared as numbers: a NaN reaches nothing), those equal to `edge` up to index `upto`
   const uint32_t bound = kth_bound(m, a.k);
-  const float least = bound == 0 ? -3.402823466e38f : key_f32(bound);      // (compared as numbers: a NaN reaches nothing)
-  // + 0: zeros of both signs are equal
-  wave_top_k<E>(E, [&](int e) { return v[e] >= least; }, [&](int e) {
-    return v[e] > -INFINITY ? ((unsigned long long)f32_key(v[e] + 0.f) << 32) | (uint32_t)~(first + (e & ~7) * 64 + lane * 8 + (e & 7)) : 0ull;
+  float least = bound == 0 ? -3.402823466e38f : key_f32(bound), edge = NAN;
+  int upto = 0;
+  const int at0 = first + lane * 8;                             // index of e: at0 + 64 (e & ~7) + (e & 7)
+  wave_top_k([&](auto f) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int off = (e & ~7) * 64 + (e & 7);
+      f(v[e] >= least && !(v[e] == edge && at0 > upto - off),
+        [&]() {
+          int at = at0;
+          asm volatile("" : "+v"(at));                          // (left to itself the compiler keeps 64 sums in registers for the few that are needed)
+          return ((unsigned long long)__float_as_uint(v[e]) << 32) | (uint32_t)(at + off);
+        });
+    }
+  }, [&]() {
+    uint32_t cur = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+      const float t = key_f32(cur | (1u << bit));               // (no number: nothing reaches it)
+      int c = 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) c += __popcll(__ballot(v[e] >= t));
+      if (c >= a.k) cur |= 1u << bit;
+    }
+    least = edge = key_f32(cur);
+    int above = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) above += __popcll(__ballot(v[e] > edge));
+    int lo = first, hi = first + 64 * E - 1;                    // the lowest index up to which enough are equal
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      int c = above;
+#pragma unroll
+      for (int e = 0; e < E; ++e) c += __popcll(__ballot(v[e] == edge && at0 <= mid - ((e & ~7) * 64 + (e & 7))));
+      if (c >= a.k) hi = mid; else lo = mid + 1;
+    }
+    upto = lo;
+  }, [&](unsigned long long r) {                                // (+ 0: zeros of both signs are equal)
+    return ((unsigned long long)f32_key(__uint_as_float((uint32_t)(r >> 32)) + 0.f) << 32) | (uint32_t)~(uint32_t)r;
   }, a.k, lists[w], a.cand + (size_t)id * a.k);
 }
 
@@ -614,16 +654,14 @@ __global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
             r[e] = e * 64 + lane < total ? src[e * 64 + lane] : 0ull;
             q[e & 3] = max(q[e & 3], (uint32_t)(r[e] >> 32));
           }
-          const uint32_t least = max(kth_bound(q, k), 1u);
-          wave_top_k<16>(16, [&](int e) { return (uint32_t)(r[e] >> 32) >= least; }, [&](int e) { return r[e]; }, k, list, keys);
+          wave_top_k_keys<16>(16, [&](int e) { return r[e]; }, kth_bound(q, k), k, list, keys);
         } else {
           auto at = [&](int e) { return e * 64 + lane < total ? src[e * 64 + lane] : 0ull; };
           const int n_e = (total + 63) / 64;
           for (int e = 0; e < n_e; e += 4)
 #pragma unroll
             for (int u = 0; u < 4; ++u) q[u] = max(q[u], (uint32_t)(at(e + u) >> 32));
-          const uint32_t least = max(kth_bound(q, k), 1u);
-          wave_top_k<1>(n_e, [&](int e) { return (uint32_t)(at(e) >> 32) >= least; }, at, k, list, keys);
+          wave_top_k_keys<1>(n_e, at, kth_bound(q, k), k, list, keys);
         }
         wave_lds_fence();
         for (int i = lane; i < k; i += 64) {
