@@ -509,42 +509,58 @@ __device__ __forceinline__ void wave_top_k_keys(const int n_e, At at, const uint
   }, [](unsigned long long x) { return x; }, k, list, out);
 }
 
-// Eight consecutive logits from index i on, in 16-byte loads wherever the row starts (rows of an odd vocabulary do not start at 16 bytes);
-// -inf beyond the row.
-__device__ __forceinline__ void load_logits(const bf16_t* x, const int i, const int n, float* v) {
-  if (i + 8 <= n) {
-    u32x4 u;
-    __builtin_memcpy(&u, x + i, 16);
+// E logits of a lane in registers, eight consecutive ones at a time, in 16-byte loads wherever the row starts (rows of an odd vocabulary do not
+// start at 16 bytes); -inf beyond the row.  bf16 logits stay packed and are unpacked in every pass over them: half the registers, so that
+// seven wavefronts share a SIMD instead of three.
+template <typename T, int E> struct UnitLogits;
+template <int E> struct UnitLogits<float, E> {
+  float v[E];
+  __device__ __forceinline__ void load(const float* x, const int e0, const int i, const int n) {
+    if (i + 8 <= n) {
+      f32x4 u[2];
+      __builtin_memcpy(u, x + i, 32);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) { v[2 * e] = __uint_as_float(u[e] << 16); v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u); }
-  } else {
+      for (int e = 0; e < 8; ++e) v[e0 + e] = u[e >> 2][e & 3];
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = i + e < n ? bf16_to_f32(x[i + e]) : -INFINITY;
+      for (int e = 0; e < 8; ++e) v[e0 + e] = i + e < n ? x[i + e] : -INFINITY;
+    }
   }
-}
-__device__ __forceinline__ void load_logits(const float* x, const int i, const int n, float* v) {
-  if (i + 8 <= n) {
-    f32x4 u[2];
-    __builtin_memcpy(u, x + i, 32);
+  __device__ __forceinline__ float operator[](int e) const { return v[e]; }
+  __device__ __forceinline__ void next_pass() {}
+};
+template <int E> struct UnitLogits<bf16_t, E> {
+  uint32_t v[E / 2];
+  __device__ __forceinline__ void load(const bf16_t* x, const int e0, const int i, const int n) {
+    if (i + 8 <= n) {
+      u32x4 u;
+      __builtin_memcpy(&u, x + i, 16);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = u[e >> 2][e & 3];
-  } else {
+      for (int e = 0; e < 4; ++e) v[e0 / 2 + e] = u[e];
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = i + e < n ? x[i + e] : -INFINITY;
+      for (int e = 0; e < 4; ++e)
+        v[e0 / 2 + e] = (i + 2 * e < n ? x[i + 2 * e] : 0xff80u) | ((uint32_t)(i + 2 * e + 1 < n ? x[i + 2 * e + 1] : 0xff80u) << 16);
+    }
   }
-}
+  __device__ __forceinline__ float operator[](int e) const { return __uint_as_float((e & 1) ? v[e >> 1] & 0xffff0000u : v[e >> 1] << 16); }
+  __device__ __forceinline__ void next_pass() {                 // what was unpacked is forgotten
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) asm volatile("" : "+v"(v[e]));
+  }
+};
 
 template <typename T, int E>
-__global__ __launch_bounds__(256) void k_beam_units(BeamSelectArgs a) {
+__global__ __launch_bounds__(256, E == 64 ? (sizeof(T) == 2 ? 5 : 3) : 8) void k_beam_units(BeamSelectArgs a) {
   __shared__ unsigned long long lists[4][BEAM_LIST];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int id = blockIdx.x * 4 + w;
   if (id >= a.n_groups * a.n_beams * a.units) return;
   const int row = id / a.units, first = (id - row * a.units) * 64 * E;
   const T* x = static_cast<const T*>(a.logits) + (size_t)row * a.ld;
-  float v[E];
+  UnitLogits<T, E> v;
 #pragma unroll
-  for (int e = 0; e < E; e += 8) load_logits(x, first + e * 64 + lane * 8, a.vocab, v + e);
+  for (int e = 0; e < E; e += 8) v.load(x, e, first + e * 64 + lane * 8, a.vocab);
   // maxima of a quarter of the lane's values each (a NaN stays out of them, and shows in the sum)
   uint32_t m[4];
   float mx = -INFINITY;
@@ -560,6 +576,7 @@ __global__ __launch_bounds__(256) void k_beam_units(BeamSelectArgs a) {
   mx = key_f32(wave_max_u32(f32_key(mx)));
   const float m_use = mx == -INFINITY ? 0.f : mx;
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  v.next_pass();
 #pragma unroll
   for (int e = 0; e < E; ++e) sum[e & 3] += __builtin_amdgcn_exp2f((v[e] - m_use) * LOG2E);
   const float total = wave_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
@@ -570,6 +587,7 @@ __global__ __launch_bounds__(256) void k_beam_units(BeamSelectArgs a) {
   int upto = 0;
   const int at0 = first + lane * 8;                             // index of e: at0 + 64 (e & ~7) + (e & 7)
   wave_top_k([&](auto f) {
+    v.next_pass();
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int off = (e & ~7) * 64 + (e & 7);
@@ -585,6 +603,7 @@ __global__ __launch_bounds__(256) void k_beam_units(BeamSelectArgs a) {
     for (int bit = 31; bit >= 0; --bit) {
       const float t = key_f32(cur | (1u << bit));               // (no number: nothing reaches it)
       int c = 0;
+      v.next_pass();
 #pragma unroll
       for (int e = 0; e < E; ++e) c += __popcll(__ballot(v[e] >= t));
       if (c >= a.k) cur |= 1u << bit;
@@ -597,6 +616,7 @@ __global__ __launch_bounds__(256) void k_beam_units(BeamSelectArgs a) {
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
       int c = above;
+      v.next_pass();
 #pragma unroll
       for (int e = 0; e < E; ++e) c += __popcll(__ballot(v[e] == edge && at0 <= mid - ((e & ~7) * 64 + (e & 7))));
       if (c >= a.k) hi = mid; else lo = mid + 1;
