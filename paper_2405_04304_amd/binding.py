@@ -332,29 +332,52 @@ def disco_draft_loop_sampled(model, kv, clf, tokens_in, n_in, cap, static_sl, po
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
-def _need(ok: bool, what: str) -> None:
-    if not ok:
-        raise DiscoError(EINVAL, what)
+def _refuse(what: str):
+    raise DiscoError(EINVAL, what)
 
 
-def _tensor(t, what: str, dtype=None, numel: Optional[int] = None, optional: bool = False):
-    """Checks what the library cannot see of a tensor: where it lives, its type, that it is contiguous, its size."""
+def _bad_tensor(t, what, dtype, numel):
+    """Says why _tensor refused (built only then: a decoding step makes these checks dozens of times)."""
     if t is None:
-        _need(optional, f"{what} is missing")
-        return
-    _need(t.is_cuda and t.device.index == torch.cuda.current_device(), f"{what} is not on the current device")
-    _need(dtype is None or t.dtype == dtype, f"{what} has type {t.dtype}, not {dtype}")
-    _need(t.is_contiguous(), f"{what} is not contiguous")
-    _need(numel is None or t.numel() >= numel, f"{what} has {t.numel()} elements, {numel} needed")
+        _refuse(f"{what} is missing")
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        _refuse(f"{what} is not on the current device")
+    if t.dtype is not dtype:
+        _refuse(f"{what} has type {t.dtype}, not {dtype}")
+    if not t.is_contiguous():
+        _refuse(f"{what} is not contiguous")
+    _refuse(f"{what} has {t.numel()} elements, {numel} needed")
 
 
-def _rows(t, what: str, n: int, width: int):
-    """(element type code, row stride) of a matrix of n rows whose columns are contiguous."""
-    _need(t.is_cuda and t.device.index == torch.cuda.current_device(), f"{what} is not on the current device")
-    _need(t.dtype in _DTYPES, f"{what} has type {t.dtype}: float32 or bfloat16")
-    _need(t.dim() == 2 and t.shape[0] >= n and t.shape[1] >= width, f"{what} has shape {tuple(t.shape)}, ({n}, {width}) needed")
-    _need(t.stride(1) == 1 or t.shape[1] == 1, f"{what}: the elements of a row are not contiguous")
-    return _DTYPES[t.dtype], max(t.stride(0), width) if n < 2 else t.stride(0)
+def _device() -> int:
+    """The current device, -1 where there is none."""
+    return torch.cuda.current_device() if torch.cuda.is_initialized() or torch.cuda.is_available() else -1
+
+
+def _tensor(t, what: str, dev: int, dtype, numel: int = 0) -> int:
+    """Address of a tensor, after the checks that the library cannot make: device, type, contiguous, size."""
+    if t is None or not t.is_cuda or t.get_device() != dev or t.dtype is not dtype or not t.is_contiguous() or t.numel() < numel:
+        _bad_tensor(t, what, dtype, numel)
+    return t.data_ptr()
+
+
+def _rows(t, what: str, dev: int, n: int, width: int):
+    """(address, element type code, row stride) of a matrix of n rows whose columns are contiguous."""
+    if not t.is_cuda or t.get_device() != dev:
+        _refuse(f"{what} is not on the current device")
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        _refuse(f"{what} has type {t.dtype}: float32 or bfloat16")
+    if t.dim() != 2 or t.shape[0] < n or t.shape[1] < width:
+        _refuse(f"{what} has shape {tuple(t.shape)}, ({n}, {width}) needed")
+    ld, one = t.stride()
+    if one != 1 and t.shape[1] != 1:
+        _refuse(f"{what}: the elements of a row are not contiguous")
+    return t.data_ptr(), code, ld if n > 1 else max(ld, t.shape[1])
+
+
+def _raw_stream(dev: int, stream) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream
 
 
 class SharedKV:
@@ -365,23 +388,29 @@ class SharedKV:
 
     def __init__(self, pages, tables, lens, page_tokens: int, n_kv_heads: int, d_head: int, prefix_pages=None, prefix_len: int = 0,
                  prefix_table=None):
-        page_shape = (2, n_kv_heads, page_tokens * d_head)
-        _tensor(pages, "pages", torch.bfloat16)
-        _need(pages.dim() == 4 and tuple(pages.shape[1:]) == page_shape, f"pages have shape {tuple(pages.shape)}, (pages, {page_shape}) needed")
-        _tensor(tables, "tables", torch.int32)
-        _need(tables.dim() == 2, "tables: [sequences, pages]")
-        _tensor(lens, "lens", torch.int32, tables.shape[0], optional=True)
+        page_shape, dev = (2, n_kv_heads, page_tokens * d_head), _device()
+        _tensor(pages, "pages", dev, torch.bfloat16)
+        if pages.dim() != 4 or tuple(pages.shape[1:]) != page_shape:
+            _refuse(f"pages have shape {tuple(pages.shape)}, (pages, {page_shape}) needed")
+        _tensor(tables, "tables", dev, torch.int32)
+        if tables.dim() != 2:
+            _refuse("tables: [sequences, pages]")
+        if lens is not None:
+            _tensor(lens, "lens", dev, torch.int32, tables.shape[0])
         n_prefix = 0
         if prefix_pages is not None:
-            _tensor(prefix_pages, "prefix_pages", torch.bfloat16)
-            _need(prefix_pages.dim() == 4 and tuple(prefix_pages.shape[1:]) == page_shape, "prefix_pages have another page shape")
+            _tensor(prefix_pages, "prefix_pages", dev, torch.bfloat16)
+            if prefix_pages.dim() != 4 or tuple(prefix_pages.shape[1:]) != page_shape:
+                _refuse("prefix_pages have another page shape")
             n_prefix = prefix_pages.shape[0]
-            _tensor(prefix_table, "prefix_table", torch.int32, -(-prefix_len // page_tokens), optional=True)
+            if prefix_table is not None:
+                _tensor(prefix_table, "prefix_table", dev, torch.int32, -(-prefix_len // page_tokens))
         self._keep = (pages, tables, lens, prefix_pages, prefix_table)
         self.lens = lens
         self.n_seqs, self.n_kv_heads, self.d_head = tables.shape[0], n_kv_heads, d_head
         self.c = SharedKVDesc(_ptr(prefix_pages), _ptr(prefix_table), n_prefix, prefix_len, _ptr(pages), _ptr(tables), _ptr(lens),
                               pages.shape[0], tables.shape[1], tables.shape[0], page_tokens, n_kv_heads, d_head)
+        self.ref = C.byref(self.c)
 
 
 def disco_rope_table(n_pos: int, d_head: int, base: float = 10000.0, device="cuda", stream=None) -> torch.Tensor:
@@ -394,23 +423,23 @@ def disco_rope_table(n_pos: int, d_head: int, base: float = 10000.0, device="cud
 def disco_append(kv: SharedKV, qkv, n_heads: int, q, seq=None, pos=None, rope=None, q_gain=None, k_gain=None, eps: float = 1e-6,
                  stream=None):
     """Keys and values of the rows of qkv into the cache, queries (normalised, rotated) to q."""
-    n, d = qkv.shape[0], kv.d_head
-    code, ld = _rows(qkv, "qkv", n, (n_heads + 2 * kv.n_kv_heads) * d)
-    code_q, ld_q = _rows(q, "q", n, n_heads * d)
-    _need(code == code_q, "q has another type than qkv")
-    for t, what in ((seq, "seq"), (pos, "pos")):
-        _tensor(t, what, torch.int32, n, optional=True)
-    _tensor(rope, "rope", torch.float32, optional=True)
-    _need(rope is None or (rope.dim() == 3 and tuple(rope.shape[1:]) == (d // 2, 2)), f"rope: [positions, {d // 2}, 2]")
-    for t, what in ((q_gain, "q_gain"), (k_gain, "k_gain")):
-        _tensor(t, what, torch.float32, d, optional=True)
-    _check(lib().disco_append(C.byref(kv.c), _ptr(qkv), code, ld, n, n_heads, _ptr(seq), _ptr(pos), _ptr(rope),
-                              rope.shape[0] if rope is not None else 0, _ptr(q_gain), _ptr(k_gain), eps, _ptr(q), ld_q,
-                              _stream() if stream is None else stream))
+    dev, n, d = _device(), qkv.shape[0], kv.d_head
+    p_qkv, code, ld = _rows(qkv, "qkv", dev, n, (n_heads + 2 * kv.n_kv_heads) * d)
+    p_q, code_q, ld_q = _rows(q, "q", dev, n, n_heads * d)
+    if code != code_q:
+        _refuse("q has another type than qkv")
+    if rope is not None and (rope.dim() != 3 or rope.shape[1] * 2 != d or rope.shape[2] != 2):
+        _refuse(f"rope: [positions, {d // 2}, 2]")
+    _check(lib().disco_append(kv.ref, p_qkv, code, ld, n, n_heads, None if seq is None else _tensor(seq, "seq", dev, torch.int32, n),
+                              None if pos is None else _tensor(pos, "pos", dev, torch.int32, n),
+                              None if rope is None else _tensor(rope, "rope", dev, torch.float32), 0 if rope is None else rope.shape[0],
+                              None if q_gain is None else _tensor(q_gain, "q_gain", dev, torch.float32, d),
+                              None if k_gain is None else _tensor(k_gain, "k_gain", dev, torch.float32, d), eps, p_q, ld_q,
+                              _raw_stream(dev, stream)))
 
 
 def disco_attn_shared_bytes(kv: SharedKV, n_tok: int, n_heads: int, max_len: int = 0) -> int:
-    n = lib().disco_attn_shared_bytes(C.byref(kv.c), n_tok, n_heads, max_len)
+    n = lib().disco_attn_shared_bytes(kv.ref, n_tok, n_heads, max_len)
     if n == 0:
         raise DiscoError(EINVAL, last_error())
     return n
@@ -419,15 +448,14 @@ def disco_attn_shared_bytes(kv: SharedKV, n_tok: int, n_heads: int, max_len: int
 def disco_attn_shared(kv: SharedKV, q, n_tok: int, n_heads: int, out, ws, lse=None, scale: Optional[float] = None, max_len: int = 0,
                       stream=None):
     """Attention of n_tok tokens of every sequence; ws: uint8, disco_attn_shared_bytes of the same arguments.  scale: d_head ** -0.5."""
-    n = kv.n_seqs * n_tok
-    code, ld = _rows(q, "q", n, n_heads * kv.d_head)
-    code_o, ld_o = _rows(out, "out", n, n_heads * kv.d_head)
-    _need(code == code_o, "out has another type than q")
-    _tensor(lse, "lse", torch.float32, n * n_heads, optional=True)
-    _tensor(ws, "ws", torch.uint8)
-    _need(kv.lens is not None or n == 0, "the cache has no lens")
-    _check(lib().disco_attn_shared(C.byref(kv.c), _ptr(q), code, ld, n_tok, n_heads, kv.d_head ** -0.5 if scale is None else scale, _ptr(out),
-                                   ld_o, _ptr(lse), max_len, _ptr(ws), ws.numel(), _stream() if stream is None else stream))
+    dev, n = _device(), kv.n_seqs * n_tok
+    p_q, code, ld = _rows(q, "q", dev, n, n_heads * kv.d_head)
+    p_out, code_o, ld_o = _rows(out, "out", dev, n, n_heads * kv.d_head)
+    if code != code_o:
+        _refuse("out has another type than q")
+    _check(lib().disco_attn_shared(kv.ref, p_q, code, ld, n_tok, n_heads, kv.d_head ** -0.5 if scale is None else scale, p_out, ld_o,
+                                   None if lse is None else _tensor(lse, "lse", dev, torch.float32, n * n_heads), max_len,
+                                   _tensor(ws, "ws", dev, torch.uint8), ws.numel(), _raw_stream(dev, stream)))
 
 
 def disco_beam_select_bytes(n_groups: int, n_beams: int, vocab: int, k: int) -> int:
@@ -440,32 +468,35 @@ def disco_beam_select_bytes(n_groups: int, n_beams: int, vocab: int, k: int) -> 
 def disco_beam_select(logits, scores, n_groups: int, n_beams: int, k: int, tokens, parents, scores_out, ws, done=None, done_out=None,
                       end_token: int = -1, stream=None):
     """The k best (beam, token) of every group; logits: [n_groups * n_beams, vocab]."""
-    n, vocab = n_groups * n_beams, logits.shape[1] if logits.dim() == 2 else 0
-    code, ld = _rows(logits, "logits", n, vocab)
-    _tensor(scores, "scores", torch.float32, n)
-    _tensor(done, "done", torch.int32, n, optional=True)
-    for t, what, dtype in ((tokens, "tokens", torch.int32), (parents, "parents", torch.int32), (scores_out, "scores_out", torch.float32)):
-        _tensor(t, what, dtype, n_groups * k)
-    _tensor(done_out, "done_out", torch.int32, n_groups * k, optional=True)
-    _tensor(ws, "ws", torch.uint8)
-    _check(lib().disco_beam_select(_ptr(logits), code, ld, n_groups, n_beams, vocab, k, _ptr(scores), _ptr(done), end_token, _ptr(tokens),
-                                   _ptr(parents), _ptr(scores_out), _ptr(done_out), _ptr(ws), ws.numel(),
-                                   _stream() if stream is None else stream))
+    dev, n, nk = _device(), n_groups * n_beams, n_groups * k
+    if logits.dim() != 2:
+        _refuse("logits: [rows, vocab]")
+    vocab = logits.shape[1]
+    p_logits, code, ld = _rows(logits, "logits", dev, n, vocab)
+    _check(lib().disco_beam_select(p_logits, code, ld, n_groups, n_beams, vocab, k, _tensor(scores, "scores", dev, torch.float32, n),
+                                   None if done is None else _tensor(done, "done", dev, torch.int32, n), end_token,
+                                   _tensor(tokens, "tokens", dev, torch.int32, nk), _tensor(parents, "parents", dev, torch.int32, nk),
+                                   _tensor(scores_out, "scores_out", dev, torch.float32, nk),
+                                   None if done_out is None else _tensor(done_out, "done_out", dev, torch.int32, nk),
+                                   _tensor(ws, "ws", dev, torch.uint8), ws.numel(), _raw_stream(dev, stream)))
 
 
 def disco_beam_reorder(pages, tables, parents, tables_out, n_groups: int, n_beams: int, length: int, page_tokens: int, stream=None):
     """Sequence b goes on from parents[b]; pages: bf16 [layers, pages, 2, n_kv_heads, page_tokens * d_head], layers may be strided."""
-    _need(pages.is_cuda and pages.device.index == torch.cuda.current_device(), "pages are not on the current device")
-    _need(pages.dim() == 5 and pages.dtype == torch.bfloat16 and pages.shape[0] > 0 and pages.shape[2] == 2 and pages[0].is_contiguous(),
-          "pages: bfloat16 [layers, pages, 2, K / V heads, page_tokens * d_head], a layer contiguous")
-    _need(pages.shape[4] % page_tokens == 0, "pages have another page size")
-    _tensor(tables, "tables", torch.int32)
-    _need(tables.dim() == 2 and tables.shape[0] >= n_groups * n_beams, "tables: [sequences, pages]")
-    _tensor(parents, "parents", torch.int32, n_groups * n_beams)
-    _tensor(tables_out, "tables_out", torch.int32, tables.numel())
-    _check(lib().disco_beam_reorder(_ptr(pages), pages.shape[0], pages.stride(0), pages.shape[1], pages[0, 0].numel(), _ptr(tables),
-                                    _ptr(tables_out), tables.shape[1], _ptr(parents), n_groups, n_beams, length, page_tokens,
-                                    _stream() if stream is None else stream))
+    dev = _device()
+    if not pages.is_cuda or pages.get_device() != dev:
+        _refuse("pages are not on the current device")
+    if pages.dim() != 5 or pages.dtype is not torch.bfloat16 or pages.shape[0] == 0 or pages.shape[2] != 2 or pages.shape[4] % page_tokens:
+        _refuse("pages: bfloat16 [layers, pages, 2, K / V heads, page_tokens * d_head]")
+    _, n_pages, _, heads, size = pages.shape
+    if pages.stride()[1:] != (2 * heads * size, heads * size, size, 1):
+        _refuse("pages: the pages of a layer are not contiguous")
+    if tables.dim() != 2 or tables.shape[0] < n_groups * n_beams:
+        _refuse("tables: [sequences, pages]")
+    _check(lib().disco_beam_reorder(pages.data_ptr(), pages.shape[0], pages.stride(0), n_pages, 2 * heads * size,
+                                    _tensor(tables, "tables", dev, torch.int32), _tensor(tables_out, "tables_out", dev, torch.int32, tables.numel()),
+                                    tables.shape[1], _tensor(parents, "parents", dev, torch.int32, n_groups * n_beams), n_groups, n_beams, length,
+                                    page_tokens, _raw_stream(dev, stream)))
 
 
 TRAIN_MAX_N = 2560
