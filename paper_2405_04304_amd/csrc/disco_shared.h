@@ -27,9 +27,9 @@ hipError_t launch_append(const AppendArgs& a, bool fp32, hipStream_t s);
 
 // Ranges and launches of an attention call.
 struct SharedAttnPlan {
-  int wr_prefix;                     // 32-row wavefronts of a workgroup over the prompt's positions (0: no prompt)
+  bool prefix_many, own_many;        // workgroups of 128 rows (else 32)
   int prefix_tiles, prefix_splits, prefix_len;    // row tiles of a kv head, ranges, positions of a range
-  int wr_own, own_tiles, own_splits, own_len;
+  int own_tiles, own_splits, own_len;
   int parts;                         // partial results of a row
   size_t bytes;                      // of the partial results (0 with one part)
 };

@@ -128,38 +128,106 @@ __device__ __forceinline__ SoftParts split_terms(const float (&x)[8]) {
 struct AttnItem {
   const bf16_t* pool; const int32_t* table; int n_pages;
   int kvh, row0, rows, part;         // row0: of the K / V head's rows
-  int begin, end;                    // positions
+  int begin, end;                    // positions; begin is a multiple of 32
   int first;                         // own positions: those below it are seen by every token of the call (prompt: end)
 };
 
-template <int DH, int WR, int WT, bool F32>
-struct AttnShape {
-  static constexpr int NW = WR * WT, NT = NW * 64, RT = 32 * WR;
-  static constexpr int TT = WT == 1 ? 64 : 32 * WT;            // positions of a tile
-  static constexpr int CK = DH / 8, S16 = DH / 16, CB = DH / 32, TERMS = F32 ? 3 : 1;
-  static constexpr int KCH = TT * CK, VCH = TT * CK;           // 16-byte chunks
-  static constexpr int OLD = DH + 4;                           // merged rows in LDS
-  static constexpr size_t stage_bytes = (size_t)(KCH + VCH) * 16;
-  static constexpr size_t merge_bytes = WT == 1 ? 0 : (size_t)WT * RT * (OLD + 2) * 4;
-  static constexpr size_t lds = stage_bytes > merge_bytes ? stage_bytes : merge_bytes;
+// A block of 32 positions in LDS, 16-byte chunks.  K: chunk c of the row in place m (position m with bits 2 and 3 swapped) at
+// m * DH / 8 + (c ^ m): the rows of a copy of 1 KiB are four consecutive positions each, and a fragment read (one chunk column) meets no bank
+// twice.  V: eight positions of a channel, half h of group g of sixteen at (g * DH + channel) * 2 + (h ^ channel / 4): a copy takes consecutive
+// bytes of a page of sixteen, a read is free of conflicts.
+template <int DH> struct AttnBlock {
+  static constexpr int CK = DH / 8, K_CHUNKS = 32 * CK, V_CHUNKS = 4 * DH, COPIES = DH / 16;     // copies (of K, of V) of a wavefront's width
 };
 
-template <int DH, int WR, int WT, bool F32>
-__device__ __forceinline__ void attn_item(const SharedAttnArgs& a, const AttnItem& it, char* lds) {
-  typedef AttnShape<DH, WR, WT, F32> Sh;
-  constexpr int CK = Sh::CK, S16 = Sh::S16, CB = Sh::CB, TT = Sh::TT, NT = Sh::NT;
-  u32x4* ks = reinterpret_cast<u32x4*>(lds);
-  u32x4* vs = ks + Sh::KCH;
-  __shared__ int s_odd;                          // a value that is not finite among V entries that not every token sees
-  const SharedKv& kv = a.kv;
-  const int pt = kv.pt, nkv = kv.nkv, grp = a.nq / nkv, T = a.n_tok;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, wr = w / WT, wt = w % WT, col = lane & 31, hf = lane >> 5;
-  const size_t head_elems = (size_t)pt * DH, page_elems = 2 * (size_t)nkv * head_elems;
+// Copies blocks of the pages into LDS.  Lanes 0 .. 7 look up the page of four positions each, lanes 8 .. 11 that of eight (V chunks).
+template <int DH>
+struct BlockCopy {
+  typedef AttnBlock<DH> Bk;
+  const AttnItem& it;
+  const SharedKv& kv;
+  size_t head_elems, page_elems;
+  int lane, bad;                     // bad: the first position this lane found in a page outside the pool
+  uint64_t addr;                     // of this lane's positions, for the block looked up last
+  int pos, entry, at;                // these positions' first, its table entry (on the way) and its place in the page
 
-  const int r_in = 32 * wr + col, r = it.row0 + min(r_in, it.rows - 1);      // this lane's row (surplus lanes repeat the last)
-  const int tok_row = r / grp, t_own = tok_row % T;
-  bf16x8 q[S16][Sh::TERMS];
-  {
+  __device__ __forceinline__ BlockCopy(const AttnItem& i, const SharedKv& k) : it(i), kv(k), head_elems((size_t)k.pt * DH), lane(threadIdx.x & 63), bad(0x7fffffff) {
+    page_elems = 2 * (size_t)k.nkv * head_elems;
+    addr = 0; pos = entry = at = 0;
+  }
+  __device__ __forceinline__ void look_up(const int base) {
+    // beyond the end: the last pieces once more (their scores and values are dropped)
+    pos = (lane & 8) ? min(base + 8 * (lane & 3), (it.end - 1) & ~7) : min(base + 4 * (lane & 7), (it.end - 1) & ~3);
+    const int lp = page_of(kv, pos);
+    entry = it.table ? it.table[lp] : lp;
+    at = pos - lp * kv.pt;
+  }
+  __device__ __forceinline__ void resolve() {
+    int page = entry;
+    if ((unsigned)page >= (unsigned)it.n_pages) { page = 0; bad = min(bad, pos); }
+    const size_t e = (size_t)page * page_elems + ((lane & 8) ? (kv.nkv + it.kvh) * head_elems + at : it.kvh * head_elems + (size_t)at * DH);
+    addr = reinterpret_cast<uint64_t>(it.pool + e);
+  }
+  __device__ __forceinline__ uint64_t lane_addr(const int l) const {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)addr, l) | ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(addr >> 32), l) << 32);
+  }
+  // copies j0 .. j1 - 1 of the block's K and V; lds_k, lds_v: addresses of the block's chunks
+  template <int J0, int J1>
+  __device__ __forceinline__ void copy(const uint32_t lds_k, const uint32_t lds_v, u32x4* v_chunks) {
+#pragma unroll
+    for (int j = J0; j < J1; ++j) {
+      if constexpr (DH == 128) {               // four rows: places 4 j .., one group of positions
+        const uint32_t off = (uint32_t)(lane >> 4) * (DH * 2) + (uint32_t)(((lane & 15) ^ (lane >> 4) ^ (4 * (j & 3))) * 16);
+        lds_dma_16(reinterpret_cast<const void*>(lane_addr((j & 4) | ((j & 1) << 1) | ((j & 2) >> 1))), off, lds_k + (uint32_t)j * 1024u);
+      } else {                                 // eight: places 8 j .., two groups
+        const int g0 = 4 * (j >> 1) + (j & 1);
+        const uint64_t b = (lane & 32) ? lane_addr(g0 + 2) : lane_addr(g0);
+        const uint32_t off = (uint32_t)((lane >> 3) & 3) * (DH * 2) + (uint32_t)(((lane & 7) ^ (lane >> 3)) * 16);
+        lds_dma_16(reinterpret_cast<const void*>(b + off), lds_k + (uint32_t)j * 1024u);
+      }
+    }
+    constexpr int PER_G = DH / 32;             // copies of sixteen positions
+    const int half = (lane ^ (lane >> 3)) & 1;
+    if ((kv.pt & 7) == 0) {
+#pragma unroll
+      for (int j = J0; j < J1; ++j) {
+        const int g = j / PER_G;
+        const uint64_t b = half ? lane_addr(8 + 2 * g + 1) : lane_addr(8 + 2 * g);
+        lds_dma_16(reinterpret_cast<const void*>(b + (uint64_t)(uint32_t)(((lane >> 1) + 32 * (j % PER_G)) * kv.pt * 2)), lds_v + (uint32_t)j * 1024u);
+      }
+    } else {                                   // a page may end after four of the eight: through registers
+#pragma unroll 1
+      for (int j = J0; j < J1; ++j) {
+        const int g = j / PER_G, ch = (lane >> 1) + 32 * (j % PER_G);
+        u32x4 v;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int grp = 4 * g + 2 * half + u;          // K's group of the same four positions, back to its V entry
+          const int off = __shfl(at, grp), e = __shfl(entry, grp);
+          const int page = (unsigned)e < (unsigned)it.n_pages ? e : 0;
+          const uint2 x = *reinterpret_cast<const uint2*>(it.pool + (size_t)page * page_elems + (kv.nkv + it.kvh) * head_elems + (size_t)ch * kv.pt + off);
+          v[2 * u] = x.x; v[2 * u + 1] = x.y;
+        }
+        v_chunks[j * 64 + lane] = v;
+      }
+    }
+  }
+};
+
+// 32 rows of a wavefront: queries, running statistics, output.
+template <int DH, bool F32>
+struct AttnRows {
+  static constexpr int CK = DH / 8, S16 = DH / 16, CB = DH / 32, TERMS = F32 ? 3 : 1;
+  bf16x8 q[S16][TERMS];
+  f32x16 O[CB];
+  float m_run, l_run, ce;
+  int col, hf, see, t_own;
+
+  __device__ __forceinline__ void init(const SharedAttnArgs& a, const AttnItem& it, const int r, const int grp) {
+    const int lane = threadIdx.x & 63;
+    col = lane & 31; hf = lane >> 5;
+    const int tok_row = r / grp;
+    t_own = tok_row % a.n_tok;
     const size_t at = (size_t)tok_row * a.ld_q + (size_t)(it.kvh * grp + r % grp) * DH + 8 * hf;
 #pragma unroll
     for (int s = 0; s < S16; ++s) {
@@ -167,230 +235,329 @@ __device__ __forceinline__ void attn_item(const SharedAttnArgs& a, const AttnIte
         const float* p = static_cast<const float*>(a.q) + at + 16 * s;
         const float4 x0 = load4(p), x1 = load4(p + 4);
         const float x[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
-        const SoftParts sp = split_terms<Sh::TERMS>(x);
+        const SoftParts sp = split_terms<TERMS>(x);
 #pragma unroll
-        for (int k = 0; k < Sh::TERMS; ++k) q[s][k] = as_bf16x8(sp.t[k]);
+        for (int k = 0; k < TERMS; ++k) q[s][k] = as_bf16x8(sp.t[k]);
       } else {
         q[s][0] = as_bf16x8(*reinterpret_cast<const u32x4*>(static_cast<const bf16_t*>(a.q) + at + 16 * s));
       }
     }
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) O[c][v] = 0.f;
+    m_run = -INFINITY; l_run = 0.f;
+    ce = a.scale * LOG2E;
+    see = min(it.end, it.first + t_own);                        // positions that this row sees
   }
-  f32x16 O[CB];
-#pragma unroll
-  for (int c = 0; c < CB; ++c)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) O[c][v] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
-  const float ce = a.scale * LOG2E;
-  const int see = min(it.end, it.first + t_own);                // positions that this row sees
-  if (tid == 0) s_odd = 0;
 
-  for (int t0 = it.begin; t0 < it.end; t0 += TT) {
-    __syncthreads();
-    for (int i = tid; i < Sh::KCH; i += NT) {                   // K: chunk c of position t0 + p
-      const int p = i / CK, c = i % CK, pos = t0 + p;
-      u32x4 v = {0u, 0u, 0u, 0u};
-      if (pos < it.end) {
-        const int lp = page_of(kv, pos), page = it.table ? it.table[lp] : lp;
-        if ((unsigned)page < (unsigned)it.n_pages)
-          v = *reinterpret_cast<const u32x4*>(it.pool + (size_t)page * page_elems + it.kvh * head_elems + (size_t)(pos - lp * pt) * DH + c * 8);
-        else
-          v = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
-      }
-      const int row = (p & ~12) | ((p & 4) << 1) | ((p & 8) >> 1);
-      ks[row * CK + (c ^ (row & (CK - 1)))] = v;
+  // 32 positions from base on, in LDS at ks, vs.  EDGE: some are not seen by every row.
+  __device__ __forceinline__ void step(const AttnItem& it, const int n_tok, const int base, const u32x4* ks, const u32x4* vs) {
+    if (base + 32 > it.first) step_of<true>(it, n_tok, base, ks, vs);
+    else step_of<false>(it, n_tok, base, ks, vs);
+  }
+  template <bool EDGE>
+  __device__ __forceinline__ void step_of(const AttnItem& it, const int n_tok, const int base, const u32x4* ks, const u32x4* vs) {
+    const u32x4* kr = ks + col * CK;
+    const u32x4* vr = vs + col * 2 + (hf ^ ((col >> 2) & 1));
+    auto k_frag = [&](const int s) { return as_bf16x8(kr[(2 * s + hf) ^ (col & (CK - 1))]); };
+    auto v_frag = [&](const int s, const int c) { return vr[(s * DH + 32 * c) * 2]; };
+    f32x16 S;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) S[v] = 0.f;
+    bf16x8 kk[3];                                               // fragments are read two steps ahead of their products
+    kk[0] = k_frag(0);
+    kk[1] = k_frag(1);
+#pragma unroll
+    for (int s = 0; s < S16; ++s) {
+      if (s + 2 < S16) kk[(s + 2) % 3] = k_frag(s + 2);
+#pragma unroll
+      for (int u = 0; u < TERMS; ++u) S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk[s % 3], q[s][u], S, 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    for (int i = tid; i < Sh::VCH; i += NT) {                   // V: eight positions of a channel
-      const int g = i / (2 * DH), ch = (i >> 1) % DH, half = i & 1, pos = t0 + 16 * g + 8 * half;
-      u32x4 v = {0u, 0u, 0u, 0u};
+    u32x4 vv[2][CB];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {                             // (a page may end after the first four)
-        const int pu = pos + 4 * u;
-        if (pu < it.end) {
-          const int lp = page_of(kv, pu), page = it.table ? it.table[lp] : lp;
-          if ((unsigned)page < (unsigned)it.n_pages) {
-            const uint2 x = *reinterpret_cast<const uint2*>(it.pool + (size_t)page * page_elems + (nkv + it.kvh) * head_elems + (size_t)ch * pt + (pu - lp * pt));
-            v[2 * u] = x.x; v[2 * u + 1] = x.y;
-          }
-        }
-      }
-      if (pos + 8 > it.first) {                                 // entries that some row does not see
-        const int n = it.end - pos;                             // entries at or beyond the end may be anything: 0 * NaN would poison the sum
-        bool odd = false;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          v[u] &= n >= 2 * u + 2 ? 0xffffffffu : (n == 2 * u + 1 ? 0xffffu : 0u);
-          odd |= (v[u] & 0x7f80u) == 0x7f80u || (v[u] & 0x7f800000u) == 0x7f800000u;
-        }
-        if (odd && it.first < it.end) s_odd = 1;
-      }
-      vs[(g * 2 + half) * DH + ch] = v;
-    }
-    __syncthreads();
-#pragma unroll 1
-    for (int b = wt; b < TT / 32; b += WT) {
-      const int base = t0 + 32 * b;
-      if (base >= it.end) break;
-      f32x16 S;
-#pragma unroll
-      for (int v = 0; v < 16; ++v) S[v] = 0.f;
-      const u32x4* kr = ks + (32 * b + col) * CK;
-#pragma unroll
-      for (int s = 0; s < S16; ++s) {
-        const bf16x8 k = as_bf16x8(kr[(2 * s + hf) ^ (col & (CK - 1))]);
-#pragma unroll
-        for (int u = 0; u < Sh::TERMS; ++u) S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[s][u], S, 0, 0, 0);
-      }
+    for (int c = 0; c < CB; ++c) vv[0][c] = v_frag(0, c);
+    if (EDGE) {
       // lane half hf holds positions base + 16 (v / 8) + 8 hf + v % 8 of its row
-      if (base + 32 > it.first) {
 #pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (base + 16 * (v >> 3) + 8 * hf + (v & 7) >= see) S[v] = -INFINITY;
-      }
-      float mx = S[0];
+      for (int v = 0; v < 16; ++v)
+        if (base + 16 * (v >> 3) + 8 * hf + (v & 7) >= see) S[v] = -INFINITY;
+    }
+    float mx = S[0];
 #pragma unroll
-      for (int v = 1; v < 16; ++v) mx = fmaxf(mx, S[v]);
-      const float m_new = fmaxf(m_run, half_max(mx) * ce);
-      const float m_use = m_new == -INFINITY ? 0.f : m_new;     // a row that sees nothing yet
+    for (int v = 1; v < 16; ++v) mx = fmaxf(mx, S[v]);
+    mx = half_max(mx) * ce;
+    // The sums stay relative to an older maximum while the new one is at most 2^8 of it: the largest terms are then below 2^8 and no sum loses
+    // precision for it, and after the first blocks almost no block rescales its output.
+    if (__builtin_amdgcn_ballot_w64(mx > m_run + 8.f) != 0ull) {
+      const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;    // (-inf: the row has seen nothing yet)
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
-      float p[16], sum = 0.f;
-#pragma unroll
-      for (int v = 0; v < 16; ++v) { p[v] = __builtin_amdgcn_exp2f(fmaf(S[v], ce, -m_use)); sum += p[v]; }
-      l_run = l_run * alpha + sum;
-      m_run = m_new;
+      l_run *= alpha;
 #pragma unroll
       for (int c = 0; c < CB; ++c)
 #pragma unroll
         for (int v = 0; v < 16; ++v) O[c][v] *= alpha;
-      const bool odd = base + 32 > it.first && s_odd != 0;
+      m_run = m_new;
+    }
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;
+    float p[16], sum[2] = {0.f, 0.f};
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const float px[8] = {p[8 * s], p[8 * s + 1], p[8 * s + 2], p[8 * s + 3], p[8 * s + 4], p[8 * s + 5], p[8 * s + 6], p[8 * s + 7]};
-        const SoftParts sp = split_terms<Sh::TERMS>(px);
-        const u32x4* vr = vs + ((2 * b + s) * 2 + hf) * DH + col;
-        if (!odd) {
+    for (int v = 0; v < 16; ++v) { p[v] = __builtin_amdgcn_exp2f(fmaf(S[v], ce, -m_use)); sum[v & 1] += p[v]; }
+    l_run += sum[0] + sum[1];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if (s == 0)
+#pragma unroll
+        for (int c = 0; c < CB; ++c) vv[1][c] = v_frag(1, c);
+      const float px[8] = {p[8 * s], p[8 * s + 1], p[8 * s + 2], p[8 * s + 3], p[8 * s + 4], p[8 * s + 5], p[8 * s + 6], p[8 * s + 7]};
+      const SoftParts sp = split_terms<TERMS>(px);
+      bool odd = false;
+      if (EDGE) {
+        // entries at or beyond the end may be anything, and 0 * NaN would poison the sum; so would an infinity or NaN that some tokens do not see
+        const int at = base + 16 * s + 8 * hf, n = it.end - at, n_all = it.first - at;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint32_t keep = n >= 2 * u + 2 ? 0xffffffffu : (n == 2 * u + 1 ? 0xffffu : 0u);
+          const uint32_t all = n_all >= 2 * u + 2 ? 0u : (n_all == 2 * u + 1 ? 0x7f800000u : 0x7f807f80u);
 #pragma unroll
           for (int c = 0; c < CB; ++c) {
-            const bf16x8 v = as_bf16x8(vr[32 * c]);
-#pragma unroll
-            for (int u = 0; u < Sh::TERMS; ++u) O[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, as_bf16x8(sp.t[u]), O[c], 0, 0, 0);
+            vv[s][c][u] &= keep;
+            const uint32_t x = vv[s][c][u] & all;
+            odd |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
           }
-        } else {
-          // an infinity or NaN that some tokens do not see: a product per token, with only what it sees, of which its rows keep the result
+        }
+        odd = __builtin_amdgcn_ballot_w64(odd) != 0ull;
+      }
+      if (!EDGE || !odd) {
+#pragma unroll
+        for (int u = 0; u < TERMS; ++u)
+#pragma unroll
+          for (int c = 0; c < CB; ++c) O[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vv[s][c]), as_bf16x8(sp.t[u]), O[c], 0, 0, 0);
+      } else {
+        // a product per token, with only what it sees, of which its rows keep the result
 #pragma unroll 1
-          for (int t = 0; t < T; ++t) {
-            const int n = it.first + t - (base + 16 * s + 8 * hf);
+        for (int t = 0; t < n_tok; ++t) {
+          const int n = it.first + t - (base + 16 * s + 8 * hf);
 #pragma unroll
-            for (int c = 0; c < CB; ++c) {
-              u32x4 v = vr[32 * c];
+          for (int c = 0; c < CB; ++c) {
+            u32x4 v = vv[s][c];
 #pragma unroll
-              for (int u = 0; u < 4; ++u) v[u] &= n >= 2 * u + 2 ? 0xffffffffu : (n == 2 * u + 1 ? 0xffffu : 0u);
-              f32x16 o = O[c];
+            for (int u = 0; u < 4; ++u) v[u] &= n >= 2 * u + 2 ? 0xffffffffu : (n == 2 * u + 1 ? 0xffffu : 0u);
+            f32x16 o = O[c];
 #pragma unroll
-              for (int u = 0; u < Sh::TERMS; ++u) o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v), as_bf16x8(sp.t[u]), o, 0, 0, 0);
+            for (int u = 0; u < TERMS; ++u) o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v), as_bf16x8(sp.t[u]), o, 0, 0, 0);
 #pragma unroll
-              for (int x = 0; x < 16; ++x) O[c][x] = t == t_own ? o[x] : O[c][x];
-            }
+            for (int x = 0; x < 16; ++x) O[c][x] = t == t_own ? o[x] : O[c][x];
+            __builtin_amdgcn_sched_barrier(0);
           }
         }
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
-  l_run = half_sum(l_run);
+};
 
-  // results of the row: to the output, or as this range's part
-  const size_t head_rows = (size_t)kv.n_seqs * T * grp;
-  auto put = [&](const int row, const int c, float4 o, const float m, const float l) {
-    const int tr = row / grp, head = it.kvh * grp + row % grp;
+// A row's result: to the output, or as this range's part.
+template <int DH, bool F32>
+struct AttnPut {
+  const SharedAttnArgs& a;
+  const AttnItem& it;
+  int grp;
+  size_t head_rows;
+  __device__ __forceinline__ AttnPut(const SharedAttnArgs& x, const AttnItem& i) : a(x), it(i), grp(x.nq / x.kv.nkv), head_rows((size_t)x.kv.n_seqs * x.n_tok * grp) {}
+  __device__ __forceinline__ void row(const int r, const int c, float4 o, const float l) const {
     if (a.plan.parts > 1) {
-      store4(a.part + (((size_t)it.part * nkv + it.kvh) * head_rows + row) * DH + c, o);
+      store4(a.part + (((size_t)it.part * a.kv.nkv + it.kvh) * head_rows + r) * DH + c, o);
       return;
     }
     const float inv = l == 0.f ? 0.f : 1.0f / l;
     o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-    if constexpr (F32) store4(static_cast<float*>(a.out) + (size_t)tr * a.ld_out + (size_t)head * DH + c, o);
-    else store4(static_cast<bf16_t*>(a.out) + (size_t)tr * a.ld_out + (size_t)head * DH + c, o);
+    const size_t at = (size_t)(r / grp) * a.ld_out + (size_t)(it.kvh * grp + r % grp) * DH + c;
+    if constexpr (F32) store4(static_cast<float*>(a.out) + at, o);
+    else store4(static_cast<bf16_t*>(a.out) + at, o);
+  }
+  __device__ __forceinline__ void stat(const int r, const float m, const float l) const {
+    if (a.plan.parts > 1) a.ml[((size_t)it.part * a.kv.nkv + it.kvh) * head_rows + r] = make_float2(m, l);
+    else if (a.lse != nullptr) a.lse[(size_t)(r / grp) * a.nq + it.kvh * grp + r % grp] = l == 0.f ? -INFINITY : (m + __log2f(l)) * LN2;
+  }
+};
+
+// 128 rows: four wavefronts of 32 that share the positions through LDS, 64 at a time in two buffers.
+template <int DH, bool F32>
+__device__ __forceinline__ void attn_many(const SharedAttnArgs& a, const AttnItem& it, char* lds) {
+  typedef AttnBlock<DH> Bk;
+  u32x4* ks = reinterpret_cast<u32x4*>(lds);                    // [buffer][block]
+  u32x4* vs = ks + 4 * Bk::K_CHUNKS;
+  __shared__ int s_bad;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  BlockCopy<DH> cp(it, a.kv);
+  const uint32_t lds_k = lds_address(ks), lds_v = lds_address(vs);
+  auto copy = [&](const int buf) {                              // of block w / 2 of a tile, half its copies
+    const int b = 2 * buf + (w >> 1);
+    cp.resolve();
+    if (w & 1) cp.template copy<Bk::COPIES / 2, Bk::COPIES>(lds_k + b * Bk::K_CHUNKS * 16, lds_v + b * Bk::V_CHUNKS * 16, vs + b * Bk::V_CHUNKS);
+    else cp.template copy<0, Bk::COPIES / 2>(lds_k + b * Bk::K_CHUNKS * 16, lds_v + b * Bk::V_CHUNKS * 16, vs + b * Bk::V_CHUNKS);
   };
-  auto put_stat = [&](const int row, const float m, const float l) {
-    if (a.plan.parts > 1) a.ml[((size_t)it.part * nkv + it.kvh) * head_rows + row] = make_float2(m, l);
-    else if (a.lse != nullptr) a.lse[(size_t)(row / grp) * a.nq + it.kvh * grp + row % grp] = l == 0.f ? -INFINITY : (m + __log2f(l)) * LN2;
+  const int mine = 32 * (w >> 1);
+  if (threadIdx.x == 0) s_bad = 0x7fffffff;
+  if (it.begin < it.end) {
+    cp.look_up(it.begin + mine);
+    copy(0);
+    if (it.begin + 64 < it.end) cp.look_up(it.begin + 64 + mine);
+  }
+  const int grp = a.nq / a.kv.nkv, r_in = 32 * w + (threadIdx.x & 31);
+  AttnRows<DH, F32> x;
+  x.init(a, it, it.row0 + min(r_in, it.rows - 1), grp);         // surplus lanes repeat the last row
+  const bool idle = 32 * w >= it.rows;
+  for (int t0 = it.begin, buf = 0; t0 < it.end; t0 += 64, buf ^= 1) {
+    // the tile has arrived and every wavefront has left the other buffer
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (t0 + 64 < it.end) {
+      copy(buf ^ 1);
+      if (t0 + 128 < it.end) cp.look_up(t0 + 128 + mine);
+    }
+#pragma unroll 1
+    for (int b = 0; b < 2; ++b) {
+      if (idle || t0 + 32 * b >= it.end) break;
+      x.step(it, a.n_tok, t0 + 32 * b, ks + (2 * buf + b) * Bk::K_CHUNKS, vs + (2 * buf + b) * Bk::V_CHUNKS);
+    }
+  }
+  __syncthreads();
+  if (cp.bad != 0x7fffffff) atomicMin(&s_bad, cp.bad);
+  __syncthreads();
+  if (r_in >= it.rows) return;
+  float l = half_sum(x.l_run);
+  if (s_bad < x.see) l = NAN;
+  const AttnPut<DH, F32> put(a, it);
+  const int r = it.row0 + r_in;
+#pragma unroll
+  for (int c = 0; c < DH / 32; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      put.row(r, 32 * c + 8 * i + 4 * x.hf, make_float4(x.O[c][4 * i], x.O[c][4 * i + 1], x.O[c][4 * i + 2], x.O[c][4 * i + 3]), l);
+  if (x.hf == 0) put.stat(r, x.m_run, l);
+}
+
+// Up to 32 rows: WT wavefronts take a block of 32 positions each in turn, copied by themselves into two buffers of their own (no barrier),
+// and put their results together at the end.
+template <int DH, int WT, bool F32>
+__device__ __forceinline__ void attn_few(const SharedAttnArgs& a, const AttnItem& it, char* lds) {
+  typedef AttnBlock<DH> Bk;
+  constexpr int OLD = DH + 4;                                   // a row put together in LDS
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31;
+  u32x4* ks = reinterpret_cast<u32x4*>(lds) + w * 2 * (Bk::K_CHUNKS + Bk::V_CHUNKS);
+  u32x4* vs = ks + 2 * Bk::K_CHUNKS;
+  BlockCopy<DH> cp(it, a.kv);
+  const uint32_t lds_k = lds_address(ks), lds_v = lds_address(vs);
+  auto copy = [&](const int buf) {
+    cp.resolve();
+    cp.template copy<0, Bk::COPIES>(lds_k + buf * Bk::K_CHUNKS * 16, lds_v + buf * Bk::V_CHUNKS * 16, vs + buf * Bk::V_CHUNKS);
   };
-  if constexpr (WT == 1) {
-    if (r_in < it.rows) {
-#pragma unroll
-      for (int c = 0; c < CB; ++c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          put(r, 32 * c + 8 * i + 4 * hf, make_float4(O[c][4 * i], O[c][4 * i + 1], O[c][4 * i + 2], O[c][4 * i + 3]), m_run, l_run);
-      if (hf == 0) put_stat(r, m_run, l_run);
+  const int t_begin = it.begin + 32 * w;
+  if (t_begin < it.end) {
+    cp.look_up(t_begin);
+    copy(0);
+    if (t_begin + 32 * WT < it.end) cp.look_up(t_begin + 32 * WT);
+  }
+  AttnRows<DH, F32> x;
+  x.init(a, it, it.row0 + min(col, it.rows - 1), a.nq / a.kv.nkv);
+  for (int t0 = t_begin, buf = 0; t0 < it.end; t0 += 32 * WT, buf ^= 1) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    if (t0 + 32 * WT < it.end) {
+      copy(buf ^ 1);
+      if (t0 + 64 * WT < it.end) cp.look_up(t0 + 64 * WT);
     }
-  } else {
-    float* sm = reinterpret_cast<float*>(lds);                  // [WT][RT] maxima, sums, then rows
-    float* sl = sm + WT * Sh::RT;
-    float* so = sl + WT * Sh::RT;
-    __syncthreads();
-    if (hf == 0) { sm[wt * Sh::RT + r_in] = m_run; sl[wt * Sh::RT + r_in] = l_run; }
-    __syncthreads();
-    float mm = sm[r_in];
+    x.step(it, a.n_tok, t0, ks + buf * Bk::K_CHUNKS, vs + buf * Bk::V_CHUNKS);
+  }
+  float* sm = reinterpret_cast<float*>(lds);                    // [WT][32] maxima, sums, first bad positions, then rows
+  float* sl = sm + WT * 32;
+  int* sb = reinterpret_cast<int*>(sl + WT * 32);
+  float* so = sl + WT * 32 + 4 * WT;
+  const float l_wave = half_sum(x.l_run);
+  int bad = cp.bad;
 #pragma unroll
-    for (int u = 1; u < WT; ++u) mm = fmaxf(mm, sm[u * Sh::RT + r_in]);
-    const float f = mm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - mm);
+  for (int o = 8; o > 0; o >>= 1) bad = min(bad, __shfl_xor(bad, o));      // (lanes 0 .. 15 look up)
+  __syncthreads();
+  if (x.hf == 0) { sm[w * 32 + col] = x.m_run; sl[w * 32 + col] = l_wave; }
+  if (lane == 0) sb[w] = bad;
+  __syncthreads();
+  float mm = sm[col];
 #pragma unroll
-    for (int c = 0; c < CB; ++c)
+  for (int u = 1; u < WT; ++u) mm = fmaxf(mm, sm[u * 32 + col]);
+  const float f = mm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.m_run - mm);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        store4(so + (size_t)(wt * Sh::RT + r_in) * Sh::OLD + 32 * c + 8 * i + 4 * hf,
-               make_float4(O[c][4 * i] * f, O[c][4 * i + 1] * f, O[c][4 * i + 2] * f, O[c][4 * i + 3] * f));
-    __syncthreads();
-    for (int i = tid; i < it.rows * (DH / 4); i += NT) {
-      const int row = i / (DH / 4), c = i % (DH / 4) * 4;
-      float m = sm[row], l = 0.f;
+  for (int c = 0; c < DH / 32; ++c)
 #pragma unroll
-      for (int u = 1; u < WT; ++u) m = fmaxf(m, sm[u * Sh::RT + row]);
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < 4; ++i)
+      store4(so + (size_t)(w * 32 + col) * OLD + 32 * c + 8 * i + 4 * x.hf,
+             make_float4(x.O[c][4 * i] * f, x.O[c][4 * i + 1] * f, x.O[c][4 * i + 2] * f, x.O[c][4 * i + 3] * f));
+  __syncthreads();
+  int first_bad = sb[0];
 #pragma unroll
-      for (int u = 0; u < WT; ++u) {
-        const float4 x = load4(so + (size_t)(u * Sh::RT + row) * Sh::OLD + c);
-        o = make_float4(o.x + x.x, o.y + x.y, o.z + x.z, o.w + x.w);
-        l += m == -INFINITY ? 0.f : sl[u * Sh::RT + row] * __builtin_amdgcn_exp2f(sm[u * Sh::RT + row] - m);
-      }
-      put(it.row0 + row, c, o, m, l);
-      if (c == 0) put_stat(it.row0 + row, m, l);
+  for (int u = 1; u < WT; ++u) first_bad = min(first_bad, sb[u]);
+  const AttnPut<DH, F32> put(a, it);
+  for (int i = threadIdx.x; i < it.rows * (DH / 4); i += 64 * WT) {
+    const int row = i / (DH / 4), c = i % (DH / 4) * 4;
+    float m = sm[row], l = 0.f;
+#pragma unroll
+    for (int u = 1; u < WT; ++u) m = fmaxf(m, sm[u * 32 + row]);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int u = 0; u < WT; ++u) {
+      const float4 y = load4(so + (size_t)(u * 32 + row) * OLD + c);
+      o = make_float4(o.x + y.x, o.y + y.y, o.z + y.z, o.w + y.w);
+      l += m == -INFINITY ? 0.f : sl[u * 32 + row] * __builtin_amdgcn_exp2f(sm[u * 32 + row] - m);
     }
+    const int r = it.row0 + row, t = r / put.grp % a.n_tok;
+    if (first_bad < min(it.end, it.first + t)) l = NAN;
+    put.row(r, c, o, l);
+    if (c == 0) put.stat(r, m, l);
   }
 }
 
-// Workgroups of the prompt's ranges first (n_prefix of them), then those of the own positions.
-template <int DH, int WR, int WT, bool F32>
-__global__ __launch_bounds__(WR * WT * 64) void k_shared_attn(SharedAttnArgs a, int n_prefix) {
-  typedef AttnShape<DH, WR, WT, F32> Sh;
-  __shared__ __align__(16) char lds[Sh::lds];
+// Workgroup b of the prompt's: ranges of a K / V head, whose row tiles go to one XCD (ids go round-robin to the eight) and so share its L2.
+__device__ __forceinline__ AttnItem prefix_item(const SharedAttnArgs& a, const int b, const int row_tile) {
   const SharedAttnPlan& p = a.plan;
   const SharedKv& kv = a.kv;
-  const int grp = a.nq / kv.nkv;
+  const int units = kv.nkv * p.prefix_splits, block = 8 * p.prefix_tiles, g = b / block, left = min(8, units - 8 * g), r = b - g * block;
+  const int tile = r / left, unit = 8 * g + r - tile * left, split = unit / kv.nkv;
   AttnItem it;
-  int b = blockIdx.x;
-  if (b < n_prefix) {
-    it.kvh = b % kv.nkv; b /= kv.nkv;
-    const int split = b % p.prefix_splits, tile = b / p.prefix_splits;
-    const int rows = kv.n_seqs * a.n_tok * grp;
-    it.pool = kv.prefix; it.table = kv.prefix_table; it.n_pages = kv.n_prefix_pages;
-    it.row0 = tile * Sh::RT; it.rows = min(Sh::RT, rows - it.row0);
-    it.begin = split * p.prefix_len; it.end = min(kv.prefix_len, it.begin + p.prefix_len); it.first = it.end;
-    it.part = split;
-  } else {
-    b -= n_prefix;
-    it.kvh = b % kv.nkv; b /= kv.nkv;
-    const int split = b % p.own_splits; b /= p.own_splits;
-    const int tile = b % p.own_tiles, seq = b / p.own_tiles;
-    const int rows = a.n_tok * grp, len = min(kv.lens[seq], kv.table_ld * kv.pt);
-    it.pool = kv.pages; it.table = kv.tables + (size_t)seq * kv.table_ld; it.n_pages = kv.n_pages;
-    it.row0 = seq * rows + tile * Sh::RT; it.rows = min(Sh::RT, rows - tile * Sh::RT);
-    it.begin = split * p.own_len; it.end = split + 1 == p.own_splits ? len : min(len, it.begin + p.own_len);
-    it.first = len - a.n_tok + 1;
-    it.part = p.prefix_splits + split;
-  }
-  attn_item<DH, WR, WT, F32>(a, it, lds);
+  it.kvh = unit - split * kv.nkv;
+  it.pool = kv.prefix; it.table = kv.prefix_table; it.n_pages = kv.n_prefix_pages;
+  it.row0 = tile * row_tile; it.rows = min(row_tile, kv.n_seqs * a.n_tok * (a.nq / kv.nkv) - it.row0);
+  it.begin = split * p.prefix_len; it.end = min(kv.prefix_len, it.begin + p.prefix_len); it.first = it.end;
+  it.part = split;
+  return it;
+}
+// Workgroup b of the own positions'.
+__device__ __forceinline__ AttnItem own_item(const SharedAttnArgs& a, int b, const int row_tile) {
+  const SharedAttnPlan& p = a.plan;
+  const SharedKv& kv = a.kv;
+  AttnItem it;
+  it.kvh = b % kv.nkv; b /= kv.nkv;
+  const int split = b % p.own_splits; b /= p.own_splits;
+  const int tile = b % p.own_tiles, seq = b / p.own_tiles;
+  const int rows = a.n_tok * (a.nq / kv.nkv), len = min(kv.lens[seq], kv.table_ld * kv.pt);
+  it.pool = kv.pages; it.table = kv.tables + (size_t)seq * kv.table_ld; it.n_pages = kv.n_pages;
+  it.row0 = seq * rows + tile * row_tile; it.rows = min(row_tile, rows - tile * row_tile);
+  it.begin = split * p.own_len; it.end = split + 1 == p.own_splits ? len : min(len, it.begin + p.own_len);
+  it.first = len - a.n_tok + 1;
+  it.part = p.prefix_splits + split;
+  return it;
+}
+
+template <int DH, bool F32>
+__global__ __launch_bounds__(256, F32 && DH == 128 ? 1 : 2) void k_attn_many(SharedAttnArgs a, int n_prefix) {
+  __shared__ __align__(16) char lds[4 * (AttnBlock<DH>::K_CHUNKS + AttnBlock<DH>::V_CHUNKS) * 16];
+  const int b = blockIdx.x;
+  attn_many<DH, F32>(a, b < n_prefix ? prefix_item(a, b, 128) : own_item(a, b - n_prefix, 128), lds);
+}
+template <int DH, int WT, bool F32>
+__global__ __launch_bounds__(64 * WT) void k_attn_few(SharedAttnArgs a, int n_prefix) {
+  __shared__ __align__(16) char lds[2 * WT * (AttnBlock<DH>::K_CHUNKS + AttnBlock<DH>::V_CHUNKS) * 16];
+  const int b = blockIdx.x;
+  attn_few<DH, WT, F32>(a, b < n_prefix ? prefix_item(a, b, 32) : own_item(a, b - n_prefix, 32), lds);
 }
 
 // The parts of a row put together: one wavefront a row.
@@ -806,54 +973,47 @@ hipError_t launch_append(const AppendArgs& a, bool fp32, hipStream_t s) {
 SharedAttnPlan shared_attn_plan(int n_seqs, int n_tok, int nq, int nkv, int dh, int prefix_len, int max_len) {
   SharedAttnPlan p{};
   const long grp = nq / nkv, own_rows = n_tok * grp, rows = n_seqs * own_rows;
-  auto ranges = [](long tiles, int len, int step, int* splits, int* range) {
-    long n = (512 + tiles - 1) / tiles;
-    const long most = (len + 255) / 256;
-    n = n < 1 ? 1 : (n > most ? (most < 1 ? 1 : most) : n);
-    if (n > 64) n = 64;
+  auto ranges = [](long tiles, int len, long want, int least, int* splits, int* range) {
+    long n = want / tiles;
+    const long most = (len + least - 1) / least;
+    n = n > most ? most : n;
+    n = n < 1 ? 1 : (n > 128 ? 128 : n);
     long r = (len + n - 1) / n;
-    r = (r + step - 1) / step * step;
-    if (r < step) r = step;
+    r = (r + 63) / 64 * 64;
+    if (r < 64) r = 64;
     *range = (int)r;
     *splits = (int)((len + r - 1) / r);
     if (*splits < 1) *splits = 1;
   };
   if (prefix_len > 0) {
-    p.wr_prefix = rows <= 32 ? 1 : (rows <= 64 ? 2 : (rows <= 128 ? 4 : 8));
-    p.prefix_tiles = (int)((rows + 32 * p.wr_prefix - 1) / (32 * p.wr_prefix));
-    ranges((long)p.prefix_tiles * nkv, prefix_len, 256, &p.prefix_splits, &p.prefix_len);
+    p.prefix_many = rows > 32;
+    p.prefix_tiles = (int)((rows + (p.prefix_many ? 127 : 31)) / (p.prefix_many ? 128 : 32));
+    ranges((long)p.prefix_tiles * nkv, prefix_len, 512, 128, &p.prefix_splits, &p.prefix_len);
   }
-  p.wr_own = own_rows <= 32 ? 1 : (own_rows <= 64 ? 2 : (own_rows <= 128 ? 4 : 8));
-  p.own_tiles = (int)((own_rows + 32 * p.wr_own - 1) / (32 * p.wr_own));
-  ranges((long)p.own_tiles * nkv * n_seqs, max_len, 256, &p.own_splits, &p.own_len);
+  p.own_many = own_rows > 32;
+  p.own_tiles = (int)((own_rows + (p.own_many ? 127 : 31)) / (p.own_many ? 128 : 32));
+  ranges((long)p.own_tiles * nkv * n_seqs, max_len, 512, 128, &p.own_splits, &p.own_len);
   p.parts = p.prefix_splits + p.own_splits;
   if (p.parts > 1) p.bytes = (size_t)p.parts * rows * nkv * (dh * sizeof(float) + sizeof(float2));
   return p;
 }
 
 template <int DH, bool F32>
-static void launch_attn_wr(int wr, unsigned n, int n_prefix, const SharedAttnArgs& a, hipStream_t s) {
-  switch (wr) {
-    case 1: hipLaunchKernelGGL((k_shared_attn<DH, 1, 4, F32>), dim3(n), dim3(256), 0, s, a, n_prefix); break;
-    case 2: hipLaunchKernelGGL((k_shared_attn<DH, 2, 2, F32>), dim3(n), dim3(256), 0, s, a, n_prefix); break;
-    case 4: hipLaunchKernelGGL((k_shared_attn<DH, 4, 1, F32>), dim3(n), dim3(256), 0, s, a, n_prefix); break;
-    default: hipLaunchKernelGGL((k_shared_attn<DH, 8, 1, F32>), dim3(n), dim3(512), 0, s, a, n_prefix); break;
-  }
-}
-
-template <int DH, bool F32>
 static hipError_t launch_attn_all(const SharedAttnArgs& a, hipStream_t s) {
   const SharedAttnPlan& p = a.plan;
   const unsigned n_prefix = (unsigned)(p.prefix_tiles * p.prefix_splits * a.kv.nkv), n_own = (unsigned)(a.kv.n_seqs * p.own_tiles * p.own_splits * a.kv.nkv);
-  if (n_prefix == 0 || p.wr_prefix == p.wr_own) {
-    launch_attn_wr<DH, F32>(p.wr_own, n_prefix + n_own, (int)n_prefix, a, s);
+  auto launch = [&](bool many, unsigned n, int prefix) {
+    if (many) hipLaunchKernelGGL((k_attn_many<DH, F32>), dim3(n), dim3(256), 0, s, a, prefix);
+    else hipLaunchKernelGGL((k_attn_few<DH, 4, F32>), dim3(n), dim3(256), 0, s, a, prefix);
+    return hipGetLastError();
+  };
+  hipError_t e;
+  if (n_prefix == 0 || p.prefix_many == p.own_many) {
+    e = launch(p.own_many, n_prefix + n_own, (int)n_prefix);
   } else {
-    launch_attn_wr<DH, F32>(p.wr_prefix, n_prefix, (int)n_prefix, a, s);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    launch_attn_wr<DH, F32>(p.wr_own, n_own, 0, a, s);
+    e = launch(p.prefix_many, n_prefix, (int)n_prefix);
+    if (e == hipSuccess) e = launch(p.own_many, n_own, 0);
   }
-  hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.parts == 1) return e;
   const size_t rows = (size_t)a.kv.n_seqs * a.n_tok * a.nq;
   constexpr int rpw = 256 / (DH / 4);
