@@ -12,6 +12,12 @@ constexpr float LOG2E = 1.44269504088896f, LN2 = 0.693147180559945f;
 
 __device__ __forceinline__ int page_of(const SharedKv& kv, int pos) { return kv.pt_shift >= 0 ? pos >> kv.pt_shift : pos / kv.pt; }
 
+// What the wavefront's lanes have written to LDS is there for all of them (the unit works in order: this only holds the compiler).
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Four consecutive elements of a row as floats, and back.
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
 __device__ __forceinline__ float4 load4(const bf16_t* p) {
@@ -181,7 +187,7 @@ struct BlockCopy {
         lds_dma_16(reinterpret_cast<const void*>(lane_addr((j & 4) | ((j & 1) << 1) | ((j & 2) >> 1))), off, lds_k + (uint32_t)j * 1024u);
       } else {                                 // eight: places 8 j .., two groups
         const int g0 = 4 * (j >> 1) + (j & 1);
-        const uint64_t b = (lane & 32) ? lane_addr(g0 + 2) : lane_addr(g0);
+        const uint64_t b0 = lane_addr(g0), b1 = lane_addr(g0 + 2), b = (lane & 32) ? b1 : b0;
         const uint32_t off = (uint32_t)((lane >> 3) & 3) * (DH * 2) + (uint32_t)(((lane & 7) ^ (lane >> 3)) * 16);
         lds_dma_16(reinterpret_cast<const void*>(b + off), lds_k + (uint32_t)j * 1024u);
       }
@@ -192,7 +198,7 @@ struct BlockCopy {
 #pragma unroll
       for (int j = J0; j < J1; ++j) {
         const int g = j / PER_G;
-        const uint64_t b = half ? lane_addr(8 + 2 * g + 1) : lane_addr(8 + 2 * g);
+        const uint64_t b0 = lane_addr(8 + 2 * g), b1 = lane_addr(8 + 2 * g + 1), b = half ? b1 : b0;
         lds_dma_16(reinterpret_cast<const void*>(b + (uint64_t)(uint32_t)(((lane >> 1) + 32 * (j % PER_G)) * kv.pt * 2)), lds_v + (uint32_t)j * 1024u);
       }
     } else {                                   // a page may end after four of the eight: through registers
@@ -214,6 +220,28 @@ struct BlockCopy {
   }
 };
 
+// V chunks i0, i0 + step, .. of a block of positions from base on that not every row sees or that lie beyond the end, put right in LDS: what is beyond
+// the end is anything, and 0 * NaN would poison the sum; so would an infinity or NaN among the newest positions, which some tokens do not see.
+// Those become 0 as well, and the result says so (add_odd gives them to the rows that do see them).
+template <int DH>
+__device__ __forceinline__ bool mend_values(const AttnItem& it, const int base, u32x4* vs, const int i0, const int step) {
+  bool odd = false;
+  for (int i = i0; i < AttnBlock<DH>::V_CHUNKS; i += step) {
+    const int ch = (i >> 1) % DH, half = (i ^ (ch >> 2)) & 1, at = base + 16 * (i / (2 * DH)) + 8 * half;
+    if (at + 8 <= it.first) continue;
+    u32x4 v = vs[i];
+    const int n = it.end - at, n_all = it.first - at;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t mask = (e & 1) ? 0xffff0000u : 0xffffu, x = v[e >> 1] & mask, inf = 0x7f807f80u & mask;
+      if (e >= n) v[e >> 1] &= ~mask;
+      else if (e >= n_all && (x & inf) == inf) { v[e >> 1] &= ~mask; odd = true; }
+    }
+    vs[i] = v;
+  }
+  return odd;
+}
+
 // 32 rows of a wavefront: queries, running statistics, output.
 template <int DH, bool F32>
 struct AttnRows {
@@ -221,13 +249,12 @@ struct AttnRows {
   bf16x8 q[S16][TERMS];
   f32x16 O[CB];
   float m_run, l_run, ce;
-  int col, hf, see, t_own;
+  int col, hf, see;
 
   __device__ __forceinline__ void init(const SharedAttnArgs& a, const AttnItem& it, const int r, const int grp) {
     const int lane = threadIdx.x & 63;
     col = lane & 31; hf = lane >> 5;
     const int tok_row = r / grp;
-    t_own = tok_row % a.n_tok;
     const size_t at = (size_t)tok_row * a.ld_q + (size_t)(it.kvh * grp + r % grp) * DH + 8 * hf;
 #pragma unroll
     for (int s = 0; s < S16; ++s) {
@@ -248,16 +275,11 @@ struct AttnRows {
       for (int v = 0; v < 16; ++v) O[c][v] = 0.f;
     m_run = -INFINITY; l_run = 0.f;
     ce = a.scale * LOG2E;
-    see = min(it.end, it.first + t_own);                        // positions that this row sees
+    see = min(it.end, it.first + tok_row % a.n_tok);            // positions that this row sees
   }
 
-  // 32 positions from base on, in LDS at ks, vs.  EDGE: some are not seen by every row.
-  __device__ __forceinline__ void step(const AttnItem& it, const int n_tok, const int base, const u32x4* ks, const u32x4* vs) {
-    if (base + 32 > it.first) step_of<true>(it, n_tok, base, ks, vs);
-    else step_of<false>(it, n_tok, base, ks, vs);
-  }
-  template <bool EDGE>
-  __device__ __forceinline__ void step_of(const AttnItem& it, const int n_tok, const int base, const u32x4* ks, const u32x4* vs) {
+  // 32 positions from base on, in LDS at ks, vs
+  __device__ __forceinline__ void step(const AttnItem& it, const int base, const u32x4* ks, const u32x4* vs) {
     const u32x4* kr = ks + col * CK;
     const u32x4* vr = vs + col * 2 + (hf ^ ((col >> 2) & 1));
     auto k_frag = [&](const int s) { return as_bf16x8(kr[(2 * s + hf) ^ (col & (CK - 1))]); };
@@ -278,7 +300,7 @@ struct AttnRows {
     u32x4 vv[2][CB];
 #pragma unroll
     for (int c = 0; c < CB; ++c) vv[0][c] = v_frag(0, c);
-    if (EDGE) {
+    if (base + 32 > it.first) {                                 // some position is not seen by every row (uniform)
       // lane half hf holds positions base + 16 (v / 8) + 8 hf + v % 8 of its row
 #pragma unroll
       for (int v = 0; v < 16; ++v)
@@ -312,48 +334,32 @@ struct AttnRows {
         for (int c = 0; c < CB; ++c) vv[1][c] = v_frag(1, c);
       const float px[8] = {p[8 * s], p[8 * s + 1], p[8 * s + 2], p[8 * s + 3], p[8 * s + 4], p[8 * s + 5], p[8 * s + 6], p[8 * s + 7]};
       const SoftParts sp = split_terms<TERMS>(px);
-      bool odd = false;
-      if (EDGE) {
-        // entries at or beyond the end may be anything, and 0 * NaN would poison the sum; so would an infinity or NaN that some tokens do not see
-        const int at = base + 16 * s + 8 * hf, n = it.end - at, n_all = it.first - at;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const uint32_t keep = n >= 2 * u + 2 ? 0xffffffffu : (n == 2 * u + 1 ? 0xffffu : 0u);
-          const uint32_t all = n_all >= 2 * u + 2 ? 0u : (n_all == 2 * u + 1 ? 0x7f800000u : 0x7f807f80u);
+      for (int u = 0; u < TERMS; ++u)
 #pragma unroll
-          for (int c = 0; c < CB; ++c) {
-            vv[s][c][u] &= keep;
-            const uint32_t x = vv[s][c][u] & all;
-            odd |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
-          }
-        }
-        odd = __builtin_amdgcn_ballot_w64(odd) != 0ull;
-      }
-      if (!EDGE || !odd) {
-#pragma unroll
-        for (int u = 0; u < TERMS; ++u)
-#pragma unroll
-          for (int c = 0; c < CB; ++c) O[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vv[s][c]), as_bf16x8(sp.t[u]), O[c], 0, 0, 0);
-      } else {
-        // a product per token, with only what it sees, of which its rows keep the result
-#pragma unroll 1
-        for (int t = 0; t < n_tok; ++t) {
-          const int n = it.first + t - (base + 16 * s + 8 * hf);
-#pragma unroll
-          for (int c = 0; c < CB; ++c) {
-            u32x4 v = vv[s][c];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) v[u] &= n >= 2 * u + 2 ? 0xffffffffu : (n == 2 * u + 1 ? 0xffffu : 0u);
-            f32x16 o = O[c];
-#pragma unroll
-            for (int u = 0; u < TERMS; ++u) o = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v), as_bf16x8(sp.t[u]), o, 0, 0, 0);
-#pragma unroll
-            for (int x = 0; x < 16; ++x) O[c][x] = t == t_own ? o[x] : O[c][x];
-            __builtin_amdgcn_sched_barrier(0);
-          }
-        }
-      }
+        for (int c = 0; c < CB; ++c) O[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vv[s][c]), as_bf16x8(sp.t[u]), O[c], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+
+  // Infinities and NaN among the values of the newest positions of this range, to the rows that see them (with whatever weight: they stay
+  // infinite); mend_values has kept them out of the sums.
+  // (share w of wt: the blocks that this wavefront takes)
+  __device__ __forceinline__ void add_odd(const SharedKv& kv, const AttnItem& it, const int w, const int wt) {
+    const int begin = max(max(it.first, it.begin), 0);
+    const size_t head_elems = (size_t)kv.pt * DH, page_elems = 2 * (size_t)kv.nkv * head_elems;
+    for (int pos = begin; pos < it.end; ++pos) {
+      if (((pos - it.begin) >> 5) % wt != w) continue;
+      const int lp = page_of(kv, pos), page = it.table ? it.table[lp] : lp;
+      if ((unsigned)page >= (unsigned)it.n_pages) continue;
+      const bf16_t* v = it.pool + (size_t)page * page_elems + (kv.nkv + it.kvh) * head_elems + (pos - lp * kv.pt);
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t x = v[(size_t)(32 * c + 8 * (i >> 2) + 4 * hf + (i & 3)) * kv.pt];
+          if (pos < see && (x & 0x7f80u) == 0x7f80u) O[c][i] += __uint_as_float(x << 16);
+        }
     }
   }
 };
@@ -389,7 +395,7 @@ __device__ __forceinline__ void attn_many(const SharedAttnArgs& a, const AttnIte
   typedef AttnBlock<DH> Bk;
   u32x4* ks = reinterpret_cast<u32x4*>(lds);                    // [buffer][block]
   u32x4* vs = ks + 4 * Bk::K_CHUNKS;
-  __shared__ int s_bad;
+  __shared__ int s_bad, s_odd;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   BlockCopy<DH> cp(it, a.kv);
   const uint32_t lds_k = lds_address(ks), lds_v = lds_address(vs);
@@ -400,7 +406,7 @@ __device__ __forceinline__ void attn_many(const SharedAttnArgs& a, const AttnIte
     else cp.template copy<0, Bk::COPIES / 2>(lds_k + b * Bk::K_CHUNKS * 16, lds_v + b * Bk::V_CHUNKS * 16, vs + b * Bk::V_CHUNKS);
   };
   const int mine = 32 * (w >> 1);
-  if (threadIdx.x == 0) s_bad = 0x7fffffff;
+  if (threadIdx.x == 0) { s_bad = 0x7fffffff; s_odd = 0; }
   if (it.begin < it.end) {
     cp.look_up(it.begin + mine);
     copy(0);
@@ -417,15 +423,20 @@ __device__ __forceinline__ void attn_many(const SharedAttnArgs& a, const AttnIte
       copy(buf ^ 1);
       if (t0 + 128 < it.end) cp.look_up(t0 + 128 + mine);
     }
+    if (t0 + 64 > it.first) {
+      if (mend_values<DH>(it, t0 + mine, vs + (2 * buf + (w >> 1)) * Bk::V_CHUNKS, threadIdx.x & 127, 128)) s_odd = 1;
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
 #pragma unroll 1
     for (int b = 0; b < 2; ++b) {
       if (idle || t0 + 32 * b >= it.end) break;
-      x.step(it, a.n_tok, t0 + 32 * b, ks + (2 * buf + b) * Bk::K_CHUNKS, vs + (2 * buf + b) * Bk::V_CHUNKS);
+      x.step(it, t0 + 32 * b, ks + (2 * buf + b) * Bk::K_CHUNKS, vs + (2 * buf + b) * Bk::V_CHUNKS);
     }
   }
   __syncthreads();
   if (cp.bad != 0x7fffffff) atomicMin(&s_bad, cp.bad);
   __syncthreads();
+  if (s_odd != 0) x.add_odd(a.kv, it, 0, 1);
   if (r_in >= it.rows) return;
   float l = half_sum(x.l_run);
   if (s_bad < x.see) l = NAN;
@@ -462,14 +473,21 @@ __device__ __forceinline__ void attn_few(const SharedAttnArgs& a, const AttnItem
   }
   AttnRows<DH, F32> x;
   x.init(a, it, it.row0 + min(col, it.rows - 1), a.nq / a.kv.nkv);
+  bool odd = false;
   for (int t0 = t_begin, buf = 0; t0 < it.end; t0 += 32 * WT, buf ^= 1) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     if (t0 + 32 * WT < it.end) {
       copy(buf ^ 1);
       if (t0 + 64 * WT < it.end) cp.look_up(t0 + 64 * WT);
     }
-    x.step(it, a.n_tok, t0, ks + buf * Bk::K_CHUNKS, vs + buf * Bk::V_CHUNKS);
+    if (t0 + 32 > it.first) {
+      odd |= mend_values<DH>(it, t0, vs + buf * Bk::V_CHUNKS, lane, 64);
+      wave_lds_fence();
+    }
+    x.step(it, t0, ks + buf * Bk::K_CHUNKS, vs + buf * Bk::V_CHUNKS);
   }
+  odd = __builtin_amdgcn_ballot_w64(odd) != 0ull;
+  if (odd) x.add_odd(a.kv, it, w, WT);
   float* sm = reinterpret_cast<float*>(lds);                    // [WT][32] maxima, sums, first bad positions, then rows
   float* sl = sm + WT * 32;
   int* sb = reinterpret_cast<int*>(sl + WT * 32);
@@ -614,12 +632,6 @@ __device__ __forceinline__ uint32_t kth_bound(const uint32_t (&m)[4], const int 
     if (n >= k) cur = t;
   }
   return cur;
-}
-
-// What the wavefront's lanes have written to LDS is there for all of them (the unit works in order: this only holds the compiler).
-__device__ __forceinline__ void wave_lds_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
 }
 
 constexpr int BEAM_LIST = 256;       // keys of a wavefront's list
