@@ -26,14 +26,17 @@ struct AppendArgs {
 hipError_t launch_append(const AppendArgs& a, bool fp32, hipStream_t s);
 
 // Ranges and launches of an attention call.
+constexpr int ATTN_MAX_PARTS = 256;
 struct SharedAttnPlan {
-  bool prefix_many, own_many;        // workgroups of 128 rows (else 32)
+  bool fused;                        // every workgroup walks the prompt before its sequence's own positions: one launch, one part
+  int few_rows;                      // rows (16 or 32) of a workgroup that is not one of 128
+  bool prefix_many, own_many;        // workgroups of 128 rows
   int prefix_tiles, prefix_splits, prefix_len;    // row tiles of a kv head, ranges, positions of a range
   int own_tiles, own_splits, own_len;
   int parts;                         // partial results of a row
   size_t bytes;                      // of the partial results (0 with one part)
 };
-SharedAttnPlan shared_attn_plan(int n_seqs, int n_tok, int nq, int nkv, int dh, int prefix_len, int max_len);
+SharedAttnPlan shared_attn_plan(int n_seqs, int n_tok, int nq, int nkv, int dh, bool fp32, int prefix_len, int max_len);
 
 struct SharedAttnArgs {
   SharedKv kv;

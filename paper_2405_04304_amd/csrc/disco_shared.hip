@@ -4,6 +4,9 @@
 #include "disco_device.h"
 #include "disco_shared.h"
 
+#include <climits>
+#include <type_traits>
+
 namespace disco {
 
 namespace {
@@ -138,83 +141,102 @@ struct AttnItem {
   int first;                         // own positions: those below it are seen by every token of the call (prompt: end)
 };
 
-// A block of 32 positions in LDS, 16-byte chunks.  K: chunk c of the row in place m (position m with bits 2 and 3 swapped) at
-// m * DH / 8 + (c ^ m): the rows of a copy of 1 KiB are four consecutive positions each, and a fragment read (one chunk column) meets no bank
-// twice.  V: eight positions of a channel, half h of group g of sixteen at (g * DH + channel) * 2 + (h ^ channel / 4): a copy takes consecutive
-// bytes of a page of sixteen, a read is free of conflicts.
+// A block of 32 positions in LDS, 16-byte chunks.  K: chunk c of the row in place m at m * DH / 8 + (c ^ m): a copy of 1 KiB is rows of four
+// consecutive positions each, and a fragment read (one chunk column of many rows) meets no bank twice.  Places: a lane's scores have to be those
+// of eight consecutive positions (see AttnRows), which are in places four apart from each other.  V: eight positions of a channel, half h of group g
+// of sixteen at (g * DH + channel) * 2 + (h ^ channel / 4): a copy takes consecutive bytes of a page of sixteen, a read is free of conflicts.
 template <int DH> struct AttnBlock {
   static constexpr int CK = DH / 8, K_CHUNKS = 32 * CK, V_CHUNKS = 4 * DH, COPIES = DH / 16;     // copies (of K, of V) of a wavefront's width
 };
+// Which four positions (of a block's eight fours) are in the four places 4 j ..
+template <int RB> __device__ __forceinline__ constexpr int four_of(int j) {
+  return RB == 32 ? (j & 4) | ((j & 1) << 1) | ((j & 2) >> 1) : ((j & 3) << 1) | (j >> 2);
+}
 
-// Copies blocks of the pages into LDS.  Lanes 0 .. 7 look up the page of four positions each, lanes 8 .. 11 that of eight (V chunks).
-template <int DH>
+// Copies blocks begin, begin + stride, .. of a range into LDS.  Lane 8 n + f looks up the page of positions 4 f .. of the n-th of eight blocks:
+// one table load and one address computation a lane for eight blocks.
+template <int DH, int RB>
 struct BlockCopy {
   typedef AttnBlock<DH> Bk;
   const AttnItem& it;
   const SharedKv& kv;
+  int begin, stride;
   size_t head_elems, page_elems;
-  int lane, bad;                     // bad: the first position this lane found in a page outside the pool
-  uint64_t addr;                     // of this lane's positions, for the block looked up last
-  int pos, entry, at;                // these positions' first, its table entry (on the way) and its place in the page
+  int bad;                           // the first position this lane found in a page outside the pool
+  uint64_t k_addr, v_addr;           // of this lane's positions
+  int pos, lp, entry;                // of the next eight blocks: positions, page of the sequence, table entry (on its way)
 
-  __device__ __forceinline__ BlockCopy(const AttnItem& i, const SharedKv& k) : it(i), kv(k), head_elems((size_t)k.pt * DH), lane(threadIdx.x & 63), bad(0x7fffffff) {
+  __device__ __forceinline__ BlockCopy(const AttnItem& i, const SharedKv& k, const int first, const int step) : it(i), kv(k), begin(first), stride(step), head_elems((size_t)k.pt * DH), bad(0x7fffffff) {
     page_elems = 2 * (size_t)k.nkv * head_elems;
-    addr = 0; pos = entry = at = 0;
+    k_addr = v_addr = 0; pos = lp = entry = 0;
   }
-  __device__ __forceinline__ void look_up(const int base) {
-    // beyond the end: the last pieces once more (their scores and values are dropped)
-    pos = (lane & 8) ? min(base + 8 * (lane & 3), (it.end - 1) & ~7) : min(base + 4 * (lane & 7), (it.end - 1) & ~3);
-    const int lp = page_of(kv, pos);
+  // table entries of blocks i .. i + 7 (beyond the end: the last pieces once more, their scores and values are dropped)
+  __device__ __forceinline__ void look_up(const int i) {
+    const int lane = threadIdx.x & 63, f = lane & 7, last = (it.end - 1) & ((f & 1) ? ~3 : ~7);
+    const long p = (long)begin + (long)(i + (lane >> 3)) * stride + 4 * f;
+    pos = p < last ? (int)p : last;
+    lp = page_of(kv, pos);
     entry = it.table ? it.table[lp] : lp;
-    at = pos - lp * kv.pt;
   }
   __device__ __forceinline__ void resolve() {
     int page = entry;
     if ((unsigned)page >= (unsigned)it.n_pages) { page = 0; bad = min(bad, pos); }
-    const size_t e = (size_t)page * page_elems + ((lane & 8) ? (kv.nkv + it.kvh) * head_elems + at : it.kvh * head_elems + (size_t)at * DH);
-    addr = reinterpret_cast<uint64_t>(it.pool + e);
+    const int off = pos - lp * kv.pt;
+    const bf16_t* base = it.pool + (size_t)page * page_elems + it.kvh * head_elems;
+    k_addr = reinterpret_cast<uint64_t>(base + (size_t)off * DH);
+    v_addr = reinterpret_cast<uint64_t>(base + kv.nkv * head_elems + off);
   }
-  __device__ __forceinline__ uint64_t lane_addr(const int l) const {
-    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)addr, l) | ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(addr >> 32), l) << 32);
+  // Before block i is copied, in order.
+  __device__ __forceinline__ void at_block(const int i) {
+    if ((i & 7) == 0) {
+      if (i == 0) look_up(0);
+      resolve();
+      look_up(i + 8);
+    }
   }
-  // copies j0 .. j1 - 1 of the block's K and V; lds_k, lds_v: addresses of the block's chunks
+  static __device__ __forceinline__ uint64_t lane_value(const uint64_t v, const int l) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, l) | ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), l) << 32);
+  }
+  // copies J0 .. J1 - 1 of block i's K to LDS address lds
   template <int J0, int J1>
-  __device__ __forceinline__ void copy(const uint32_t lds_k, const uint32_t lds_v, u32x4* v_chunks) {
+  __device__ __forceinline__ void copy_k(const int i, const uint32_t lds) const {
+    const int lane = threadIdx.x & 63, n = 8 * (i & 7);
 #pragma unroll
     for (int j = J0; j < J1; ++j) {
-      if constexpr (DH == 128) {               // four rows: places 4 j .., one group of positions
-        const uint32_t off = (uint32_t)(lane >> 4) * (DH * 2) + (uint32_t)(((lane & 15) ^ (lane >> 4) ^ (4 * (j & 3))) * 16);
-        lds_dma_16(reinterpret_cast<const void*>(lane_addr((j & 4) | ((j & 1) << 1) | ((j & 2) >> 1))), off, lds_k + (uint32_t)j * 1024u);
-      } else {                                 // eight: places 8 j .., two groups
-        const int g0 = 4 * (j >> 1) + (j & 1);
-        const uint64_t b0 = lane_addr(g0), b1 = lane_addr(g0 + 2), b = (lane & 32) ? b1 : b0;
-        const uint32_t off = (uint32_t)((lane >> 3) & 3) * (DH * 2) + (uint32_t)(((lane & 7) ^ (lane >> 3)) * 16);
-        lds_dma_16(reinterpret_cast<const void*>(b + off), lds_k + (uint32_t)j * 1024u);
+      if constexpr (DH == 128) {               // four rows
+        const uint32_t at = (uint32_t)(lane >> 4) * (DH * 2) + (uint32_t)(((lane & 15) ^ (lane >> 4) ^ (4 * (j & 3))) * 16);
+        lds_dma_16(reinterpret_cast<const void*>(lane_value(k_addr, n + four_of<RB>(j))), at, lds + (uint32_t)j * 1024u);
+      } else {                                 // eight, of two fours
+        const uint64_t b0 = lane_value(k_addr, n + four_of<RB>(2 * j)), b1 = lane_value(k_addr, n + four_of<RB>(2 * j + 1));
+        const uint32_t at = (uint32_t)((lane >> 3) & 3) * (DH * 2) + (uint32_t)(((lane & 7) ^ (lane >> 3)) * 16);
+        lds_dma_16(reinterpret_cast<const void*>(((lane & 32) ? b1 : b0) + at), lds + (uint32_t)j * 1024u);
       }
     }
+  }
+  // ... and of its V, to LDS address lds of chunks v
+  template <int J0, int J1>
+  __device__ __forceinline__ void copy_v(const int i, const uint32_t lds, u32x4* v) const {
     constexpr int PER_G = DH / 32;             // copies of sixteen positions
-    const int half = (lane ^ (lane >> 3)) & 1;
+    const int lane = threadIdx.x & 63, n = 8 * (i & 7), half = (lane ^ (lane >> 3)) & 1;
+    const uint64_t row = (uint64_t)(uint32_t)((lane >> 1) * kv.pt * 2);
     if ((kv.pt & 7) == 0) {
+      uint64_t b = 0;
 #pragma unroll
       for (int j = J0; j < J1; ++j) {
-        const int g = j / PER_G;
-        const uint64_t b0 = lane_addr(8 + 2 * g), b1 = lane_addr(8 + 2 * g + 1), b = half ? b1 : b0;
-        lds_dma_16(reinterpret_cast<const void*>(b + (uint64_t)(uint32_t)(((lane >> 1) + 32 * (j % PER_G)) * kv.pt * 2)), lds_v + (uint32_t)j * 1024u);
+        if (j == J0 || j % PER_G == 0) {
+          const uint64_t b0 = lane_value(v_addr, n + 4 * (j / PER_G)), b1 = lane_value(v_addr, n + 4 * (j / PER_G) + 2);
+          b = (half ? b1 : b0) + row;
+        }
+        lds_dma_16(reinterpret_cast<const void*>(b + (uint64_t)(64 * (j % PER_G)) * kv.pt), lds + (uint32_t)j * 1024u);
       }
     } else {                                   // a page may end after four of the eight: through registers
-#pragma unroll 1
-      for (int j = J0; j < J1; ++j) {
-        const int g = j / PER_G, ch = (lane >> 1) + 32 * (j % PER_G);
-        u32x4 v;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int grp = 4 * g + 2 * half + u;          // K's group of the same four positions, back to its V entry
-          const int off = __shfl(at, grp), e = __shfl(entry, grp);
-          const int page = (unsigned)e < (unsigned)it.n_pages ? e : 0;
-          const uint2 x = *reinterpret_cast<const uint2*>(it.pool + (size_t)page * page_elems + (kv.nkv + it.kvh) * head_elems + (size_t)ch * kv.pt + off);
-          v[2 * u] = x.x; v[2 * u + 1] = x.y;
-        }
-        v_chunks[j * 64 + lane] = v;
+      for (int j = J0; j < J1; ++j) {
+        uint64_t b[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) b[u] = lane_value(v_addr, n + 4 * (j / PER_G) + u) + row + (uint64_t)(64 * (j % PER_G)) * kv.pt;
+        const uint2 x = *reinterpret_cast<const uint2*>(half ? b[2] : b[0]), y = *reinterpret_cast<const uint2*>(half ? b[3] : b[1]);
+        v[j * 64 + lane] = u32x4{x.x, x.y, y.x, y.y};
       }
     }
   }
@@ -242,74 +264,118 @@ __device__ __forceinline__ bool mend_values(const AttnItem& it, const int base, 
   return odd;
 }
 
-// 32 rows of a wavefront: queries, running statistics, output.
-template <int DH, bool F32>
+// RB (16 or 32) rows of a wavefront: queries, running statistics, output.  A lane's scores are those of its row and, eight at a time, of consecutive
+// positions: 32 rows, 32x32x16 products: positions 16 n + 8 (lane / 32) + 0 .. 7; 16 rows, 16x16x32 products: positions 8 (lane / 16) + 0 .. 7.
+// Those are what the second product wants of the lane, so the probabilities never leave it.
+template <int DH, int RB, bool F32>
 struct AttnRows {
-  static constexpr int CK = DH / 8, S16 = DH / 16, CB = DH / 32, TERMS = F32 ? 3 : 1;
-  bf16x8 q[S16][TERMS];
-  f32x16 O[CB];
+  typedef typename std::conditional<RB == 32, f32x16, f32x4>::type Acc;
+  static constexpr int CK = DH / 8, TERMS = F32 ? 3 : 1;
+  static constexpr int STEPS = RB == 32 ? DH / 16 : DH / 32;   // products over the channels
+  static constexpr int CB = DH / RB, AV = RB == 32 ? 16 : 4;   // channel tiles of the output, values of one
+  static constexpr int NS = RB == 32 ? 16 : 8, SV = NS / 8;    // scores of a lane in a block
+  bf16x8 q[STEPS][TERMS];
+  Acc O[CB];
   float m_run, l_run, ce;
-  int col, hf, see;
+  int col, hf, tok, see;                                        // row, part of the wavefront, token of the call, positions of the range that the row sees
 
-  __device__ __forceinline__ void init(const SharedAttnArgs& a, const AttnItem& it, const int r, const int grp) {
-    const int lane = threadIdx.x & 63;
-    col = lane & 31; hf = lane >> 5;
-    const int tok_row = r / grp;
-    const size_t at = (size_t)tok_row * a.ld_q + (size_t)(it.kvh * grp + r % grp) * DH + 8 * hf;
+  // The queries as they lie in memory: requested first, turned into terms (init) when the first copies are on their way.
+  struct Raw { u32x4 v[STEPS * (F32 ? 2 : 1)]; };
+  static __device__ __forceinline__ Raw request(const SharedAttnArgs& a, const AttnItem& it, const int r, const int grp) {
+    Raw q;
+    const size_t at = (size_t)(r / grp) * a.ld_q + (size_t)(it.kvh * grp + r % grp) * DH + 8 * ((threadIdx.x & 63) / RB);
+    constexpr int W = DH / STEPS;
 #pragma unroll
-    for (int s = 0; s < S16; ++s) {
+    for (int s = 0; s < STEPS; ++s) {
       if constexpr (F32) {
-        const float* p = static_cast<const float*>(a.q) + at + 16 * s;
-        const float4 x0 = load4(p), x1 = load4(p + 4);
-        const float x[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
-        const SoftParts sp = split_terms<TERMS>(x);
+        const u32x4* p = reinterpret_cast<const u32x4*>(static_cast<const float*>(a.q) + at + W * s);
+        q.v[2 * s] = p[0]; q.v[2 * s + 1] = p[1];
+      } else {
+        q.v[s] = *reinterpret_cast<const u32x4*>(static_cast<const bf16_t*>(a.q) + at + W * s);
+      }
+    }
+    return q;
+  }
+  __device__ __forceinline__ void init(const SharedAttnArgs& a, const AttnItem& it, const Raw& raw, const int r, const int grp) {
+    const int lane = threadIdx.x & 63;
+    col = lane & (RB - 1); hf = lane / RB;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      if constexpr (F32) {
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = __uint_as_float(raw.v[2 * s + (i >> 2)][i & 3]);
+        const SoftParts sp = split_terms<TERMS>(y);
 #pragma unroll
         for (int k = 0; k < TERMS; ++k) q[s][k] = as_bf16x8(sp.t[k]);
       } else {
-        q[s][0] = as_bf16x8(*reinterpret_cast<const u32x4*>(static_cast<const bf16_t*>(a.q) + at + 16 * s));
+        q[s][0] = as_bf16x8(raw.v[s]);
       }
     }
 #pragma unroll
     for (int c = 0; c < CB; ++c)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) O[c][v] = 0.f;
+      for (int v = 0; v < AV; ++v) O[c][v] = 0.f;
     m_run = -INFINITY; l_run = 0.f;
     ce = a.scale * LOG2E;
-    see = min(it.end, it.first + tok_row % a.n_tok);            // positions that this row sees
+    tok = r / grp % a.n_tok;
+    see = min(it.end, it.first + tok);
   }
+  static __device__ __forceinline__ Acc product(const bf16x8 x, const bf16x8 y, const Acc c) {
+    if constexpr (RB == 32) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ float row_max(float x) { if constexpr (RB == 32) return half_max(x); else return row4_max(x); }
+  __device__ __forceinline__ float row_sum() const { if constexpr (RB == 32) return half_sum(l_run); else return row4_sum(l_run); }
+  // channel of value v of output tile c
+  __device__ __forceinline__ int channel(const int c, const int v) const { return RB == 32 ? 32 * c + 8 * (v >> 2) + 4 * hf + (v & 3) : 16 * c + 4 * hf + v; }
 
-  // 32 positions from base on, in LDS at ks, vs
-  __device__ __forceinline__ void step(const AttnItem& it, const int base, const u32x4* ks, const u32x4* vs) {
-    const u32x4* kr = ks + col * CK;
-    const u32x4* vr = vs + col * 2 + (hf ^ ((col >> 2) & 1));
-    auto k_frag = [&](const int s) { return as_bf16x8(kr[(2 * s + hf) ^ (col & (CK - 1))]); };
-    auto v_frag = [&](const int s, const int c) { return vr[(s * DH + 32 * c) * 2]; };
-    f32x16 S;
+  template <int NB> struct Scores { float s[NB * NS]; };
+  // scores of NB blocks of 32 positions in LDS at ks
+  template <int NB>
+  __device__ __forceinline__ Scores<NB> scores(const u32x4* ks) const {
+    Scores<NB> r;
+    constexpr int TILES = 32 / RB * NB, AHEAD = 4, N = STEPS * TILES;      // tiles of places; fragments are read AHEAD of their products
+    Acc S[TILES];
+    auto k_frag = [&](const int i) {
+      const int place = i % TILES * RB + col;
+      return as_bf16x8(ks[place * CK + ((64 / RB * (i / TILES) + hf) ^ (place & (CK - 1)))]);
+    };
+    bf16x8 kk[AHEAD + 1];
 #pragma unroll
-    for (int v = 0; v < 16; ++v) S[v] = 0.f;
-    bf16x8 kk[3];                                               // fragments are read two steps ahead of their products
-    kk[0] = k_frag(0);
-    kk[1] = k_frag(1);
+    for (int i = 0; i < AHEAD; ++i) kk[i] = k_frag(i);
 #pragma unroll
-    for (int s = 0; s < S16; ++s) {
-      if (s + 2 < S16) kk[(s + 2) % 3] = k_frag(s + 2);
+    for (int i = 0; i < N; ++i) {
+      if (i + AHEAD < N) kk[(i + AHEAD) % (AHEAD + 1)] = k_frag(i + AHEAD);
 #pragma unroll
-      for (int u = 0; u < TERMS; ++u) S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk[s % 3], q[s][u], S, 0, 0, 0);
+      for (int u = 0; u < TERMS; ++u) {
+        if (i < TILES && u == 0) {
+          Acc z;
+#pragma unroll
+          for (int v = 0; v < AV; ++v) z[v] = 0.f;
+          S[i % TILES] = product(kk[i % (AHEAD + 1)], q[0][0], z);
+        } else {
+          S[i % TILES] = product(kk[i % (AHEAD + 1)], q[i / TILES][u], S[i % TILES]);
+        }
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
-    u32x4 vv[2][CB];
 #pragma unroll
-    for (int c = 0; c < CB; ++c) vv[0][c] = v_frag(0, c);
-    if (base + 32 > it.first) {                                 // some position is not seen by every row (uniform)
-      // lane half hf holds positions base + 16 (v / 8) + 8 hf + v % 8 of its row
+    for (int v = 0; v < NB * NS; ++v) r.s[v] = S[v / AV][v % AV];
+    return r;
+  }
+  // Probabilities (relative to the running maximum) of the positions from base on, in place of their scores.
+  template <int NB>
+  __device__ __forceinline__ void weigh(const AttnItem& it, const int base, Scores<NB>& S) {
+    if (base + 32 * NB > it.first) {                            // some position is not seen by every row (uniform)
 #pragma unroll
-      for (int v = 0; v < 16; ++v)
-        if (base + 16 * (v >> 3) + 8 * hf + (v & 7) >= see) S[v] = -INFINITY;
+      for (int v = 0; v < NB * NS; ++v)
+        if (base + 32 * (v / NS) + 16 * (v % NS >> 3) + 8 * hf + (v & 7) >= see) S.s[v] = -INFINITY;
     }
-    float mx = S[0];
+    float mx = S.s[0];
 #pragma unroll
-    for (int v = 1; v < 16; ++v) mx = fmaxf(mx, S[v]);
-    mx = half_max(mx) * ce;
+    for (int v = 1; v < NB * NS; ++v) mx = fmaxf(mx, S.s[v]);
+    mx = row_max(mx) * ce;
     // The sums stay relative to an older maximum while the new one is at most 2^8 of it: the largest terms are then below 2^8 and no sum loses
     // precision for it, and after the first blocks almost no block rescales its output.
     if (__builtin_amdgcn_ballot_w64(mx > m_run + 8.f) != 0ull) {
@@ -319,32 +385,43 @@ struct AttnRows {
 #pragma unroll
       for (int c = 0; c < CB; ++c)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) O[c][v] *= alpha;
+        for (int v = 0; v < AV; ++v) O[c][v] *= alpha;
       m_run = m_new;
     }
     const float m_use = m_run == -INFINITY ? 0.f : m_run;
-    float p[16], sum[2] = {0.f, 0.f};
+    float sum[2] = {0.f, 0.f};
 #pragma unroll
-    for (int v = 0; v < 16; ++v) { p[v] = __builtin_amdgcn_exp2f(fmaf(S[v], ce, -m_use)); sum[v & 1] += p[v]; }
+    for (int v = 0; v < NB * NS; ++v) { S.s[v] = __builtin_amdgcn_exp2f(fmaf(S.s[v], ce, -m_use)); sum[v & 1] += S.s[v]; }
     l_run += sum[0] + sum[1];
+  }
+  // output += values in LDS at vs, weighted
+  template <int NB>
+  __device__ __forceinline__ void add(const u32x4* vs, const Scores<NB>& P) {
+    constexpr int N = NB * SV;
+    u32x4 vv[2][CB];
+    auto v_frag = [&](const int s, const int c) {
+      const int ch = RB * c + col, g = RB == 32 ? s : 2 * s + (hf >> 1), half = RB == 32 ? hf : hf & 1;
+      return vs[(g * DH + ch) * 2 + (half ^ ((col >> 2) & 1))];
+    };
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      if (s == 0)
+    for (int c = 0; c < CB; ++c) vv[0][c] = v_frag(0, c);
 #pragma unroll
-        for (int c = 0; c < CB; ++c) vv[1][c] = v_frag(1, c);
-      const float px[8] = {p[8 * s], p[8 * s + 1], p[8 * s + 2], p[8 * s + 3], p[8 * s + 4], p[8 * s + 5], p[8 * s + 6], p[8 * s + 7]};
+    for (int s = 0; s < N; ++s) {
+      if (s + 1 < N)
+#pragma unroll
+        for (int c = 0; c < CB; ++c) vv[(s + 1) & 1][c] = v_frag(s + 1, c);
+      const float px[8] = {P.s[8 * s], P.s[8 * s + 1], P.s[8 * s + 2], P.s[8 * s + 3], P.s[8 * s + 4], P.s[8 * s + 5], P.s[8 * s + 6], P.s[8 * s + 7]};
       const SoftParts sp = split_terms<TERMS>(px);
 #pragma unroll
       for (int u = 0; u < TERMS; ++u)
 #pragma unroll
-        for (int c = 0; c < CB; ++c) O[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vv[s][c]), as_bf16x8(sp.t[u]), O[c], 0, 0, 0);
+        for (int c = 0; c < CB; ++c) O[c] = product(as_bf16x8(vv[s & 1][c]), as_bf16x8(sp.t[u]), O[c]);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
 
   // Infinities and NaN among the values of the newest positions of this range, to the rows that see them (with whatever weight: they stay
-  // infinite); mend_values has kept them out of the sums.
-  // (share w of wt: the blocks that this wavefront takes)
+  // infinite); mend_values has kept them out of the sums.  (share w of wt: the blocks that this wavefront takes)
   __device__ __forceinline__ void add_odd(const SharedKv& kv, const AttnItem& it, const int w, const int wt) {
     const int begin = max(max(it.first, it.begin), 0);
     const size_t head_elems = (size_t)kv.pt * DH, page_elems = 2 * (size_t)kv.nkv * head_elems;
@@ -356,8 +433,8 @@ struct AttnRows {
 #pragma unroll
       for (int c = 0; c < CB; ++c)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const uint32_t x = v[(size_t)(32 * c + 8 * (i >> 2) + 4 * hf + (i & 3)) * kv.pt];
+        for (int i = 0; i < AV; ++i) {
+          const uint32_t x = v[(size_t)channel(c, i) * kv.pt];
           if (pos < see && (x & 0x7f80u) == 0x7f80u) O[c][i] += __uint_as_float(x << 16);
         }
     }
@@ -396,41 +473,42 @@ __device__ __forceinline__ void attn_many(const SharedAttnArgs& a, const AttnIte
   u32x4* ks = reinterpret_cast<u32x4*>(lds);                    // [buffer][block]
   u32x4* vs = ks + 4 * Bk::K_CHUNKS;
   __shared__ int s_bad, s_odd;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  BlockCopy<DH> cp(it, a.kv);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = 32 * (w >> 1);
+  BlockCopy<DH, 32> cp(it, a.kv, it.begin + mine, 64);
   const uint32_t lds_k = lds_address(ks), lds_v = lds_address(vs);
-  auto copy = [&](const int buf) {                              // of block w / 2 of a tile, half its copies
-    const int b = 2 * buf + (w >> 1);
-    cp.resolve();
-    if (w & 1) cp.template copy<Bk::COPIES / 2, Bk::COPIES>(lds_k + b * Bk::K_CHUNKS * 16, lds_v + b * Bk::V_CHUNKS * 16, vs + b * Bk::V_CHUNKS);
-    else cp.template copy<0, Bk::COPIES / 2>(lds_k + b * Bk::K_CHUNKS * 16, lds_v + b * Bk::V_CHUNKS * 16, vs + b * Bk::V_CHUNKS);
+  auto copy = [&](const int i) {                                // tile i: of block w / 2, half its copies
+    const int b = 2 * (i & 1) + (w >> 1);
+    constexpr int H = Bk::COPIES / 2;
+    cp.at_block(i);
+    if (w & 1) {
+      cp.template copy_k<H, Bk::COPIES>(i, lds_k + b * Bk::K_CHUNKS * 16);
+      cp.template copy_v<H, Bk::COPIES>(i, lds_v + b * Bk::V_CHUNKS * 16, vs + b * Bk::V_CHUNKS);
+    } else {
+      cp.template copy_k<0, H>(i, lds_k + b * Bk::K_CHUNKS * 16);
+      cp.template copy_v<0, H>(i, lds_v + b * Bk::V_CHUNKS * 16, vs + b * Bk::V_CHUNKS);
+    }
   };
-  const int mine = 32 * (w >> 1);
   if (threadIdx.x == 0) { s_bad = 0x7fffffff; s_odd = 0; }
-  if (it.begin < it.end) {
-    cp.look_up(it.begin + mine);
-    copy(0);
-    if (it.begin + 64 < it.end) cp.look_up(it.begin + 64 + mine);
-  }
-  const int grp = a.nq / a.kv.nkv, r_in = 32 * w + (threadIdx.x & 31);
-  AttnRows<DH, F32> x;
-  x.init(a, it, it.row0 + min(r_in, it.rows - 1), grp);         // surplus lanes repeat the last row
+  const int grp = a.nq / a.kv.nkv, r_in = 32 * w + (threadIdx.x & 31), r_mine = it.row0 + min(r_in, it.rows - 1);    // surplus lanes repeat the last row
+  AttnRows<DH, 32, F32> x;
+  const auto raw = x.request(a, it, r_mine, grp);
+  const int tiles = it.begin < it.end ? (it.end - it.begin + 63) / 64 : 0;
+  if (tiles > 0) copy(0);
+  x.init(a, it, raw, r_mine, grp);
   const bool idle = 32 * w >= it.rows;
-  for (int t0 = it.begin, buf = 0; t0 < it.end; t0 += 64, buf ^= 1) {
+  for (int i = 0; i < tiles; ++i) {
+    const int t0 = it.begin + 64 * i, buf = i & 1;
     // the tile has arrived and every wavefront has left the other buffer
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (t0 + 64 < it.end) {
-      copy(buf ^ 1);
-      if (t0 + 128 < it.end) cp.look_up(t0 + 128 + mine);
-    }
+    if (i + 1 < tiles) copy(i + 1);
     if (t0 + 64 > it.first) {
       if (mend_values<DH>(it, t0 + mine, vs + (2 * buf + (w >> 1)) * Bk::V_CHUNKS, threadIdx.x & 127, 128)) s_odd = 1;
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
-#pragma unroll 1
-    for (int b = 0; b < 2; ++b) {
-      if (idle || t0 + 32 * b >= it.end) break;
-      x.step(it, t0 + 32 * b, ks + (2 * buf + b) * Bk::K_CHUNKS, vs + (2 * buf + b) * Bk::V_CHUNKS);
+    if (!idle) {
+      auto S = x.template scores<2>(ks + 2 * buf * Bk::K_CHUNKS);
+      x.weigh(it, t0, S);
+      x.add(vs + 2 * buf * Bk::V_CHUNKS, S);
     }
   }
   __syncthreads();
@@ -438,94 +516,116 @@ __device__ __forceinline__ void attn_many(const SharedAttnArgs& a, const AttnIte
   __syncthreads();
   if (s_odd != 0) x.add_odd(a.kv, it, 0, 1);
   if (r_in >= it.rows) return;
-  float l = half_sum(x.l_run);
+  float l = x.row_sum();
   if (s_bad < x.see) l = NAN;
   const AttnPut<DH, F32> put(a, it);
   const int r = it.row0 + r_in;
 #pragma unroll
-  for (int c = 0; c < DH / 32; ++c)
+  for (int c = 0; c < x.CB; ++c)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      put.row(r, 32 * c + 8 * i + 4 * x.hf, make_float4(x.O[c][4 * i], x.O[c][4 * i + 1], x.O[c][4 * i + 2], x.O[c][4 * i + 3]), l);
+    for (int i = 0; i < 16; i += 4) put.row(r, x.channel(c, i), make_float4(x.O[c][i], x.O[c][i + 1], x.O[c][i + 2], x.O[c][i + 3]), l);
   if (x.hf == 0) put.stat(r, x.m_run, l);
 }
 
-// Up to 32 rows: WT wavefronts take a block of 32 positions each in turn, copied by themselves into two buffers of their own (no barrier),
-// and put their results together at the end.
-template <int DH, int WT, bool F32>
-__device__ __forceinline__ void attn_few(const SharedAttnArgs& a, const AttnItem& it, char* lds) {
+// Up to RB rows: WT wavefronts take a block of 32 positions each in turn, copied by themselves into a K and a V buffer of their own (no barrier): the
+// next block's K is on its way from the scores on, its V from the output on, and other wavefronts of the SIMD cover what is left of the wait.
+// Results are put together at the end.  `also`: a second range for the same rows, walked first (pool == nullptr: none).
+template <int DH, int RB, int WT, bool F32> struct FewShape {
   typedef AttnBlock<DH> Bk;
-  constexpr int OLD = DH + 4;                                   // a row put together in LDS
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31;
-  u32x4* ks = reinterpret_cast<u32x4*>(lds) + w * 2 * (Bk::K_CHUNKS + Bk::V_CHUNKS);
-  u32x4* vs = ks + 2 * Bk::K_CHUNKS;
-  BlockCopy<DH> cp(it, a.kv);
+  static constexpr int OLD = DH + 4;                            // a row put together in LDS
+  static constexpr size_t stage = (size_t)WT * (Bk::K_CHUNKS + Bk::V_CHUNKS) * 16, merge = (size_t)(WT * RB * (OLD + 2) + 4 * WT) * 4;
+  static constexpr size_t lds = stage > merge ? stage : merge;
+};
+template <int DH, int RB, int WT, bool F32>
+__device__ __forceinline__ void attn_few(const SharedAttnArgs& a, const AttnItem& it, const AttnItem& also, char* lds) {
+  typedef AttnBlock<DH> Bk;
+  constexpr int OLD = FewShape<DH, RB, WT, F32>::OLD;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = threadIdx.x & (RB - 1), lane = threadIdx.x & 63;
+  u32x4* ks = reinterpret_cast<u32x4*>(lds) + w * (Bk::K_CHUNKS + Bk::V_CHUNKS);
+  u32x4* vs = ks + Bk::K_CHUNKS;
   const uint32_t lds_k = lds_address(ks), lds_v = lds_address(vs);
-  auto copy = [&](const int buf) {
-    cp.resolve();
-    cp.template copy<0, Bk::COPIES>(lds_k + buf * Bk::K_CHUNKS * 16, lds_v + buf * Bk::V_CHUNKS * 16, vs + buf * Bk::V_CHUNKS);
-  };
-  const int t_begin = it.begin + 32 * w;
-  if (t_begin < it.end) {
-    cp.look_up(t_begin);
-    copy(0);
-    if (t_begin + 32 * WT < it.end) cp.look_up(t_begin + 32 * WT);
-  }
-  AttnRows<DH, F32> x;
-  x.init(a, it, it.row0 + min(col, it.rows - 1), a.nq / a.kv.nkv);
-  bool odd = false;
-  for (int t0 = t_begin, buf = 0; t0 < it.end; t0 += 32 * WT, buf ^= 1) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    if (t0 + 32 * WT < it.end) {
-      copy(buf ^ 1);
-      if (t0 + 64 * WT < it.end) cp.look_up(t0 + 64 * WT);
+  const int r_mine = it.row0 + min(col, it.rows - 1);
+  AttnRows<DH, RB, F32> x;
+  const auto raw = x.request(a, it, r_mine, a.nq / a.kv.nkv);
+  bool started = false;
+  auto walk = [&](const AttnItem& seg) {                        // the first position of seg in a page outside the pool
+    BlockCopy<DH, RB> cp(seg, a.kv, seg.begin + 32 * w, 32 * WT);
+    const int n = seg.end > cp.begin ? (seg.end - cp.begin + 32 * WT - 1) / (32 * WT) : 0;    // blocks
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // (reads of the range before)
+    if (n > 0) {
+      cp.at_block(0);
+      cp.template copy_k<0, Bk::COPIES>(0, lds_k);
+      cp.template copy_v<0, Bk::COPIES>(0, lds_v, vs);
     }
-    if (t0 + 32 > it.first) {
-      odd |= mend_values<DH>(it, t0, vs + buf * Bk::V_CHUNKS, lane, 64);
-      wave_lds_fence();
+    if (!started) x.init(a, it, raw, r_mine, a.nq / a.kv.nkv);
+    started = true;
+    x.see = min(seg.end, seg.first + x.tok);
+    bool odd = false;
+    for (int i = 0; i < n; ++i) {
+      const int t0 = cp.begin + i * cp.stride;
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(Bk::COPIES) : "memory");     // its K (V's copies were sent later)
+      auto S = x.template scores<1>(ks);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (i + 1 < n) {
+        cp.at_block(i + 1);
+        cp.template copy_k<0, Bk::COPIES>(i + 1, lds_k);
+      }
+      x.weigh(seg, t0, S);
+      if (i + 1 < n) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(Bk::COPIES) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      if (t0 + 32 > seg.first) {
+        odd |= mend_values<DH>(seg, t0, vs, lane, 64);
+        wave_lds_fence();
+      }
+      x.add(vs, S);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (i + 1 < n) cp.template copy_v<0, Bk::COPIES>(i + 1, lds_v, vs);
     }
-    x.step(it, t0, ks + buf * Bk::K_CHUNKS, vs + buf * Bk::V_CHUNKS);
-  }
-  odd = __builtin_amdgcn_ballot_w64(odd) != 0ull;
-  if (odd) x.add_odd(a.kv, it, w, WT);
-  float* sm = reinterpret_cast<float*>(lds);                    // [WT][32] maxima, sums, first bad positions, then rows
-  float* sl = sm + WT * 32;
-  int* sb = reinterpret_cast<int*>(sl + WT * 32);
-  float* so = sl + WT * 32 + 4 * WT;
-  const float l_wave = half_sum(x.l_run);
-  int bad = cp.bad;
+    odd = __builtin_amdgcn_ballot_w64(odd) != 0ull;
+    if (odd) x.add_odd(a.kv, seg, w, WT);
+    int bad = cp.bad;
 #pragma unroll
-  for (int o = 8; o > 0; o >>= 1) bad = min(bad, __shfl_xor(bad, o));      // (lanes 0 .. 15 look up)
+    for (int o = 32; o > 0; o >>= 1) bad = min(bad, __shfl_xor(bad, o));
+    return bad;
+  };
+  int bad = 0x7fffffff;                                         // of `it`; in front of all positions: one of `also`
+  if (also.pool != nullptr && walk(also) != 0x7fffffff) bad = INT_MIN;
+  bad = min(bad, walk(it));
+  const float l_wave = x.row_sum();
+  const AttnPut<DH, F32> put(a, it);
+  constexpr int AV = AttnRows<DH, RB, F32>::AV, CB = AttnRows<DH, RB, F32>::CB;
+  float* sm = reinterpret_cast<float*>(lds);                    // [WT][RB] maxima, sums, first bad positions, then rows
+  float* sl = sm + WT * RB;
+  int* sb = reinterpret_cast<int*>(sl + WT * RB);
+  float* so = sl + WT * RB + 4 * WT;
   __syncthreads();
-  if (x.hf == 0) { sm[w * 32 + col] = x.m_run; sl[w * 32 + col] = l_wave; }
+  if (x.hf == 0) { sm[w * RB + col] = x.m_run; sl[w * RB + col] = l_wave; }
   if (lane == 0) sb[w] = bad;
   __syncthreads();
   float mm = sm[col];
 #pragma unroll
-  for (int u = 1; u < WT; ++u) mm = fmaxf(mm, sm[u * 32 + col]);
+  for (int u = 1; u < WT; ++u) mm = fmaxf(mm, sm[u * RB + col]);
   const float f = mm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.m_run - mm);
 #pragma unroll
-  for (int c = 0; c < DH / 32; ++c)
+  for (int c = 0; c < CB; ++c)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      store4(so + (size_t)(w * 32 + col) * OLD + 32 * c + 8 * i + 4 * x.hf,
-             make_float4(x.O[c][4 * i] * f, x.O[c][4 * i + 1] * f, x.O[c][4 * i + 2] * f, x.O[c][4 * i + 3] * f));
+    for (int i = 0; i < AV; i += 4)
+      store4(so + (size_t)(w * RB + col) * OLD + x.channel(c, i), make_float4(x.O[c][i] * f, x.O[c][i + 1] * f, x.O[c][i + 2] * f, x.O[c][i + 3] * f));
   __syncthreads();
   int first_bad = sb[0];
 #pragma unroll
   for (int u = 1; u < WT; ++u) first_bad = min(first_bad, sb[u]);
-  const AttnPut<DH, F32> put(a, it);
   for (int i = threadIdx.x; i < it.rows * (DH / 4); i += 64 * WT) {
     const int row = i / (DH / 4), c = i % (DH / 4) * 4;
     float m = sm[row], l = 0.f;
 #pragma unroll
-    for (int u = 1; u < WT; ++u) m = fmaxf(m, sm[u * 32 + row]);
+    for (int u = 1; u < WT; ++u) m = fmaxf(m, sm[u * RB + row]);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int u = 0; u < WT; ++u) {
-      const float4 y = load4(so + (size_t)(u * 32 + row) * OLD + c);
+      const float4 y = load4(so + (size_t)(u * RB + row) * OLD + c);
       o = make_float4(o.x + y.x, o.y + y.y, o.z + y.z, o.w + y.w);
-      l += m == -INFINITY ? 0.f : sl[u * 32 + row] * __builtin_amdgcn_exp2f(sm[u * 32 + row] - m);
+      l += m == -INFINITY ? 0.f : sl[u * RB + row] * __builtin_amdgcn_exp2f(sm[u * RB + row] - m);
     }
     const int r = it.row0 + row, t = r / put.grp % a.n_tok;
     if (first_bad < min(it.end, it.first + t)) l = NAN;
@@ -571,41 +671,74 @@ __global__ __launch_bounds__(256, F32 && DH == 128 ? 1 : 2) void k_attn_many(Sha
   const int b = blockIdx.x;
   attn_many<DH, F32>(a, b < n_prefix ? prefix_item(a, b, 128) : own_item(a, b - n_prefix, 128), lds);
 }
-template <int DH, int WT, bool F32>
-__global__ __launch_bounds__(64 * WT) void k_attn_few(SharedAttnArgs a, int n_prefix) {
-  __shared__ __align__(16) char lds[2 * WT * (AttnBlock<DH>::K_CHUNKS + AttnBlock<DH>::V_CHUNKS) * 16];
+// fused: a workgroup walks the prompt itself before its sequence's own positions
+template <int DH, int RB, int WT, bool F32>
+__global__ __launch_bounds__(64 * WT, RB == 32 && DH == 128 ? 1 : 2) void k_attn_few(SharedAttnArgs a, int n_prefix) {
+  __shared__ __align__(16) char lds[FewShape<DH, RB, WT, F32>::lds];
   const int b = blockIdx.x;
-  attn_few<DH, WT, F32>(a, b < n_prefix ? prefix_item(a, b, 32) : own_item(a, b - n_prefix, 32), lds);
+  const AttnItem it = b < n_prefix ? prefix_item(a, b, RB) : own_item(a, b - n_prefix, RB);
+  AttnItem also = it;
+  also.pool = nullptr;
+  if (a.plan.fused) {
+    also.pool = a.kv.prefix; also.table = a.kv.prefix_table; also.n_pages = a.kv.n_prefix_pages;
+    also.begin = 0; also.end = also.first = a.kv.prefix_len;
+  }
+  attn_few<DH, RB, WT, F32>(a, it, also, lds);
 }
 
-// The parts of a row put together: one wavefront a row.
+// The parts of a row put together.  DH / 4 lanes a row: first every lane takes statistics of some parts, then its four channels of all of them,
+// eight parts on their way at once.  Bound by the round trips: parts come from other XCDs' stores, through the memory-side cache.
 template <int DH, bool F32>
 __global__ __launch_bounds__(256) void k_shared_merge(SharedAttnArgs a) {
-  constexpr int LPR = DH / 4, RPW = 256 / LPR;
+  constexpr int LPR = DH / 4, RPW = 256 / LPR, PPL = ATTN_MAX_PARTS / LPR;
+  __shared__ float s_f[RPW][ATTN_MAX_PARTS];
   const SharedKv& kv = a.kv;
-  const int grp = a.nq / kv.nkv;
+  const int grp = a.nq / kv.nkv, parts = a.plan.parts, me = threadIdx.x % LPR, wr = threadIdx.x / LPR;
   const size_t head_rows = (size_t)kv.n_seqs * a.n_tok * grp, total = head_rows * kv.nkv;
-  const size_t i = (size_t)blockIdx.x * RPW + threadIdx.x / LPR;
-  if (i >= total) return;
-  const int c = (threadIdx.x % LPR) * 4;
-  float m = -INFINITY;
-  for (int p = 0; p < a.plan.parts; ++p) m = fmaxf(m, a.ml[p * total + i].x);
+  const size_t i = (size_t)blockIdx.x * RPW + wr;
+  if (i >= total) return;                                       // (a row's lanes are of one wavefront)
+  float2 st[PPL];
+  float m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int u = 0; u < PPL; ++u) {
+    st[u] = make_float2(-INFINITY, 0.f);
+    if (u * LPR + me < parts) st[u] = a.ml[(size_t)(u * LPR + me) * total + i];
+  }
+#pragma unroll
+  for (int u = 0; u < PPL; ++u) m = fmaxf(m, st[u].x);
+#pragma unroll
+  for (int o = 1; o < LPR; o *= 2) m = fmaxf(m, __shfl_xor(m, o));
+#pragma unroll
+  for (int u = 0; u < PPL; ++u) {
+    // a part of which the row sees nothing has sum 0 and weighs nothing
+    const float f = st[u].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(st[u].x - m);
+    if (st[u].y != 0.f) l += st[u].y * f;
+    if (u * LPR + me < parts) s_f[wr][u * LPR + me] = f;
+  }
+#pragma unroll
+  for (int o = 1; o < LPR; o *= 2) l += __shfl_xor(l, o);
+  wave_lds_fence();
+  const float* part = a.part + i * DH + me * 4;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  float l = 0.f;
-  for (int p = 0; p < a.plan.parts; ++p) {
-    const float2 s = a.ml[p * total + i];
-    if (s.y == 0.f) continue;                                   // a range of which the row sees nothing
-    const float f = __builtin_amdgcn_exp2f(s.x - m);
-    const float4 x = load4(a.part + (p * total + i) * DH + c);
-    l += s.y * f;
-    o = make_float4(fmaf(x.x, f, o.x), fmaf(x.y, f, o.y), fmaf(x.z, f, o.z), fmaf(x.w, f, o.w));
+  for (int p = 0; p < parts; p += 8) {
+    float4 x[8];
+    float f[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int q = min(p + u, parts - 1);
+      x[u] = load4(part + (size_t)q * total * DH);
+      f[u] = p + u < parts ? s_f[wr][q] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (f[u] != 0.f) o = make_float4(fmaf(x[u].x, f[u], o.x), fmaf(x[u].y, f[u], o.y), fmaf(x[u].z, f[u], o.z), fmaf(x[u].w, f[u], o.w));
   }
   const int kvh = (int)(i / head_rows), row = (int)(i % head_rows), tr = row / grp, head = kvh * grp + row % grp;
   const float inv = l == 0.f ? 0.f : 1.0f / l;
   o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-  if constexpr (F32) store4(static_cast<float*>(a.out) + (size_t)tr * a.ld_out + (size_t)head * DH + c, o);
-  else store4(static_cast<bf16_t*>(a.out) + (size_t)tr * a.ld_out + (size_t)head * DH + c, o);
-  if (c == 0 && a.lse != nullptr) a.lse[(size_t)tr * a.nq + head] = l == 0.f ? -INFINITY : (m + __log2f(l)) * LN2;
+  if constexpr (F32) store4(static_cast<float*>(a.out) + (size_t)tr * a.ld_out + (size_t)head * DH + me * 4, o);
+  else store4(static_cast<bf16_t*>(a.out) + (size_t)tr * a.ld_out + (size_t)head * DH + me * 4, o);
+  if (me == 0 && a.lse != nullptr) a.lse[(size_t)tr * a.nq + head] = l == 0.f ? -INFINITY : (m + __log2f(l)) * LN2;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -982,14 +1115,26 @@ hipError_t launch_append(const AppendArgs& a, bool fp32, hipStream_t s) {
   return hipGetLastError();
 }
 
-SharedAttnPlan shared_attn_plan(int n_seqs, int n_tok, int nq, int nkv, int dh, int prefix_len, int max_len) {
+// Which rows share a workgroup, and how the positions are cut into ranges.  Up to 32 rows a K / V head (or a sequence) has: workgroups of that
+// many rows and two wavefronts, ranges of at least 128 positions, as many as give every compute unit one workgroup (eight beams of 40 heads, 2048
+// positions: 256 wanted 20 us, 512 21, 1024 25; four wavefronts 23, one 25).  More rows: 128 a workgroup, ranges of at least 256 positions for
+// two workgroups a compute unit (one where registers allow no more), but one where a range would then have no more than 512 positions: what is
+// gained is less than what the additional parts cost (4608 rows over 3001 positions: 28 us with one, 32 with two; 384 over 65537: 245 and 193).
+// A prompt and own positions that four wavefronts walk in two steps take one launch, every sequence reading the prompt by itself: 100 + 20
+// positions of 12 heads 7.9 us against 9.9, but 523 + 37 for four sequences 13.2 against 10.4.
+SharedAttnPlan shared_attn_plan(int n_seqs, int n_tok, int nq, int nkv, int dh, bool fp32, int prefix_len, int max_len) {
   SharedAttnPlan p{};
   const long grp = nq / nkv, own_rows = n_tok * grp, rows = n_seqs * own_rows;
-  auto ranges = [](long tiles, int len, long want, int least, int* splits, int* range) {
-    long n = want / tiles;
-    const long most = (len + least - 1) / least;
-    n = n > most ? most : n;
-    n = n < 1 ? 1 : (n > 128 ? 128 : n);
+  auto ranges = [&](bool many, long tiles, int len, int* splits, int* range) {
+    const int least = many ? 256 : 128;
+    auto cut = [&](long want) {
+      long n = want / tiles;
+      const long most = ((long)len + least - 1) / least;
+      n = n > most ? most : n;
+      return n < 1 ? 1 : (n > ATTN_MAX_PARTS / 2 ? ATTN_MAX_PARTS / 2 : n);
+    };
+    long n = cut(256);
+    if (many && !(fp32 && dh == 128) && len > 512 * n) n = cut(512);
     long r = (len + n - 1) / n;
     r = (r + 63) / 64 * 64;
     if (r < 64) r = 64;
@@ -997,14 +1142,20 @@ SharedAttnPlan shared_attn_plan(int n_seqs, int n_tok, int nq, int nkv, int dh, 
     *splits = (int)((len + r - 1) / r);
     if (*splits < 1) *splits = 1;
   };
-  if (prefix_len > 0) {
-    p.prefix_many = rows > 32;
-    p.prefix_tiles = (int)((rows + (p.prefix_many ? 127 : 31)) / (p.prefix_many ? 128 : 32));
-    ranges((long)p.prefix_tiles * nkv, prefix_len, 512, 128, &p.prefix_splits, &p.prefix_len);
-  }
   p.own_many = own_rows > 32;
-  p.own_tiles = (int)((own_rows + (p.own_many ? 127 : 31)) / (p.own_many ? 128 : 32));
-  ranges((long)p.own_tiles * nkv * n_seqs, max_len, 512, 128, &p.own_splits, &p.own_len);
+  p.own_tiles = p.own_many ? (int)((own_rows + 127) / 128) : 1;
+  p.fused = prefix_len > 0 && !p.own_many && (long)prefix_len + max_len <= 256;
+  if (p.fused) {
+    p.own_splits = 1; p.own_len = max_len;
+  } else {
+    if (prefix_len > 0) {
+      p.prefix_many = rows > 32;
+      p.prefix_tiles = p.prefix_many ? (int)((rows + 127) / 128) : 1;
+      ranges(p.prefix_many, (long)p.prefix_tiles * nkv, prefix_len, &p.prefix_splits, &p.prefix_len);
+    }
+    ranges(p.own_many, (long)p.own_tiles * nkv * n_seqs, max_len, &p.own_splits, &p.own_len);
+  }
+  p.few_rows = (p.prefix_tiles > 0 && !p.prefix_many ? rows : own_rows) <= 16 ? 16 : 32;
   p.parts = p.prefix_splits + p.own_splits;
   if (p.parts > 1) p.bytes = (size_t)p.parts * rows * nkv * (dh * sizeof(float) + sizeof(float2));
   return p;
@@ -1016,7 +1167,10 @@ static hipError_t launch_attn_all(const SharedAttnArgs& a, hipStream_t s) {
   const unsigned n_prefix = (unsigned)(p.prefix_tiles * p.prefix_splits * a.kv.nkv), n_own = (unsigned)(a.kv.n_seqs * p.own_tiles * p.own_splits * a.kv.nkv);
   auto launch = [&](bool many, unsigned n, int prefix) {
     if (many) hipLaunchKernelGGL((k_attn_many<DH, F32>), dim3(n), dim3(256), 0, s, a, prefix);
-    else hipLaunchKernelGGL((k_attn_few<DH, 4, F32>), dim3(n), dim3(256), 0, s, a, prefix);
+    else if (p.few_rows == 16 && p.fused) hipLaunchKernelGGL((k_attn_few<DH, 16, 4, F32>), dim3(n), dim3(256), 0, s, a, prefix);
+    else if (p.few_rows == 16) hipLaunchKernelGGL((k_attn_few<DH, 16, 2, F32>), dim3(n), dim3(128), 0, s, a, prefix);
+    else if (p.fused) hipLaunchKernelGGL((k_attn_few<DH, 32, 4, F32>), dim3(n), dim3(256), 0, s, a, prefix);
+    else hipLaunchKernelGGL((k_attn_few<DH, 32, 2, F32>), dim3(n), dim3(128), 0, s, a, prefix);
     return hipGetLastError();
   };
   hipError_t e;

@@ -72,9 +72,9 @@ int check_attn(const disco_shared_kv* kv, int n_tok, int n_heads, int max_len) {
   return DISCO_OK;
 }
 
-SharedAttnPlan attn_plan(const disco_shared_kv* kv, int n_tok, int n_heads, int max_len) {
+SharedAttnPlan attn_plan(const disco_shared_kv* kv, bool fp32, int n_tok, int n_heads, int max_len) {
   const int cap = kv->table_ld * kv->page_tokens;
-  return shared_attn_plan(kv->n_seqs, n_tok, n_heads, kv->n_kv_heads, kv->d_head, kv->prefix_len, max_len == 0 || max_len > cap ? cap : max_len);
+  return shared_attn_plan(kv->n_seqs, n_tok, n_heads, kv->n_kv_heads, kv->d_head, fp32, kv->prefix_len, max_len == 0 || max_len > cap ? cap : max_len);
 }
 
 bool launchable(const disco_shared_kv* kv, const SharedAttnPlan& p) {
@@ -126,7 +126,11 @@ int disco_append(const disco_shared_kv* kv, const void* dev_qkv, int dtype, int6
 
 size_t disco_attn_shared_bytes(const disco_shared_kv* kv, int n_tok, int n_heads, int max_len) {
   if (check_attn(kv, n_tok, n_heads, max_len)) return 0;
-  const size_t n = kv->n_seqs ? attn_plan(kv, n_tok, n_heads, max_len).bytes : 0;
+  size_t n = 0;                      // (the two types' plans differ: room for either)
+  for (int fp32 = 0; kv->n_seqs && fp32 < 2; ++fp32) {
+    const size_t m = attn_plan(kv, fp32 != 0, n_tok, n_heads, max_len).bytes;
+    n = m > n ? m : n;
+  }
   return round_up(n < 256 ? 256 : n, 256);
 }
 
@@ -145,7 +149,7 @@ int disco_attn_shared(const disco_shared_kv* kv, const void* dev_q, int dtype, i
   if (overlap(dev_q, es * ((size_t)ld_q * (n_rows - 1) + width), dev_out, es * ((size_t)ld_out * (n_rows - 1) + width)))
     return fail(DISCO_EINVAL, "dev_out overlaps dev_q");
   SharedAttnArgs a{};
-  a.plan = attn_plan(kv, n_tok, n_heads, max_len);
+  a.plan = attn_plan(kv, dtype == DISCO_F32, n_tok, n_heads, max_len);
   if (!launchable(kv, a.plan)) return fail(DISCO_EINVAL, "more workgroups than a launch takes");
   if (a.plan.bytes > 0) {
     if (!dev_ws || !aligned(dev_ws, 256)) return fail(DISCO_EINVAL, "workspace null or not 256-byte aligned");

@@ -19,6 +19,9 @@ def _kv(**over):
     return B.SharedKVDesc(**d)
 
 
+LONG = dict(prefix_len=1000, n_prefix_pages=63)
+
+
 BAD_SHAPES = [dict(d_head=96), dict(d_head=0), dict(page_tokens=6), dict(page_tokens=0), dict(n_kv_heads=0), dict(n_seqs=-1), dict(n_seqs=65536),
               dict(prefix_len=-1), dict(n_prefix_pages=-1), dict(table_ld=0), dict(n_pages=0), dict(table_ld=1 << 30)]
 
@@ -60,11 +63,14 @@ def _attn(kv=None, **over):
 
 
 def test_attention_refusals():
-    need = B.lib().disco_attn_shared_bytes(C.byref(_kv()), 1, 4, 0)
+    assert B.lib().disco_attn_shared_bytes(C.byref(_kv()), 1, 4, 0) == 256            # one launch, no parts
+    need = B.lib().disco_attn_shared_bytes(C.byref(_kv(**LONG)), 1, 4, 0)
     assert need > 256
+    assert _attn(_kv(**LONG), ws_bytes=need - 1024) == B.EINVAL and "workspace" in B.last_error()
+    assert _attn(_kv(**LONG), ws=None) == B.EINVAL and _attn(_kv(**LONG), ws=FAKE + 6 * GB + 128) == B.EINVAL
     for over in (dict(n_tok=0), dict(n_tok=17), dict(n_heads=3), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")),
                  dict(max_len=-1), dict(q=None), dict(out=None), dict(q=FAKE + 4), dict(out=FAKE + 4), dict(ld_q=252), dict(ld_out=258), dict(dtype=7),
-                 dict(out=FAKE + 4 * GB), dict(ws=None), dict(ws=FAKE + 6 * GB + 128), dict(ws_bytes=256), dict(lse=FAKE + 2)):
+                 dict(out=FAKE + 4 * GB), dict(lse=FAKE + 2)):
         assert _attn(**over) == B.EINVAL, over
     for over in (dict(dev_prefix=None), dict(dev_prefix=FAKE + 8), dict(dev_prefix_table=FAKE + 2), dict(dev_lens=None), dict(dev_pages=None), dict(dev_tables=None)):
         assert _attn(_kv(**over)) == B.EINVAL, over
@@ -72,7 +78,7 @@ def test_attention_refusals():
 
 
 def test_attention_workspace_follows_the_plan():
-    size = lambda n_tok=1, heads=4, max_len=0, **over: B.lib().disco_attn_shared_bytes(C.byref(_kv(**over)), n_tok, heads, max_len)  # noqa: E731
+    size = lambda n_tok=1, heads=4, max_len=0, **over: B.lib().disco_attn_shared_bytes(C.byref(_kv(**{**LONG, **over})), n_tok, heads, max_len)  # noqa: E731
     assert size(prefix_len=0, table_ld=1) == 256                     # one range: nothing to put together
     assert size(n_tok=2) > size() and size(heads=8) > size()
     assert size(n_seqs=0) == 256
