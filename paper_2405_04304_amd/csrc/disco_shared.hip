@@ -52,50 +52,172 @@ __device__ __forceinline__ RowPlace row_place(const AppendArgs& a, int i) {
   return r;
 }
 
-// y_h = rotate(norm(x_h)) for query and key heads, v as it is.  DH / 8 lanes hold a head of a row: four channels of the first half and
-// their rotary partners in the second.
-template <int DH, typename T>
-__global__ __launch_bounds__(256) void k_append(AppendArgs a) {
-  constexpr int LPR = DH / 8, RPW = 256 / LPR;
-  const int i = blockIdx.x * RPW + threadIdx.x / LPR, c = (threadIdx.x % LPR) * 4, h = blockIdx.y;
+// N (4 or 8) consecutive elements of a row as floats, and floats as elements of a row.
+template <int N, typename T>
+__device__ __forceinline__ void load_piece(const T* p, float (&v)[N]) {
+  if constexpr (N == 8 && sizeof(T) == 2) {
+    const u32x4 x = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(x[i] << 16); v[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u); }
+  } else {
+    static_assert(N == 4, "16 bytes at most");
+    const float4 x = load4(p);
+    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+  }
+}
+template <int N, typename T>
+__device__ __forceinline__ void store_piece(T* p, const float (&v)[N]) {
+  if constexpr (N == 8) *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+  else store4(p, make_float4(v[0], v[1], v[2], v[3]));
+}
+
+// Queries and keys: y = rotate(norm(x)).  A lane holds N elements of a row's first half of a head and their rotary partners in the second; its
+// (cos, sin) stay in registers over HB heads of the row, whose loads are on their way together.  In calls of few rows the values' heads
+// come here as well, one entry at a time into their transposed blocks.
+template <typename T, int HB> constexpr int append_piece = HB > 1 && sizeof(T) == 2 ? 8 : 4;      // (16 bytes; few rows take what gives more wavefronts)
+template <int DH, typename T, int HB>
+__device__ __forceinline__ void append_heads(const AppendArgs& a, const int row_block, const int h0) {
+  constexpr int N = append_piece<T, HB>, LPR = DH / 2 / N, RPW = 256 / LPR;
+  const SharedKv& kv = a.kv;
+  const int i = row_block * RPW + threadIdx.x / LPR, c = threadIdx.x % LPR * N, heads = a.nq + (HB == 1 ? 2 : 1) * kv.nkv;
+  float lo[HB][N], hi[HB][N];
+  if (i < a.rows) {
+    const T* x = static_cast<const T*>(a.qkv) + (size_t)i * a.ld + c;
+#pragma unroll
+    for (int u = 0; u < HB; ++u) {
+      const int h = min(h0 + u, heads - 1);
+      load_piece(x + h * DH, lo[u]);
+      load_piece(x + h * DH + DH / 2, hi[u]);
+    }
+  }
   const RowPlace at = row_place(a, i);
   if (at.pos < 0) return;
-  const SharedKv& kv = a.kv;
-  const T* x = static_cast<const T*>(a.qkv) + (size_t)i * a.ld + (size_t)h * DH;
-  float4 lo = load4(x + c), hi = load4(x + DH / 2 + c);
+  float cs[N], sn[N];
+  if (a.rope != nullptr) {
+    const float* t = a.rope + ((size_t)(kv.prefix_len + at.pos) * (DH / 2) + c) * 2;
+#pragma unroll
+    for (int e = 0; e < N; e += 2) {
+      const float4 p = load4(t + 2 * e);
+      cs[e] = p.x; sn[e] = p.y; cs[e + 1] = p.z; sn[e + 1] = p.w;
+    }
+  }
   const int off = at.pos - page_of(kv, at.pos) * kv.pt;
-  if (h < a.nq + kv.nkv) {
+#pragma unroll
+  for (int u = 0; u < HB; ++u) {
+    const int h = h0 + u;
+    if (h >= heads) break;
+    if (HB == 1 && h >= a.nq + kv.nkv) {
+      if (at.page < 0) break;
+      bf16_t* v = kv.pages + ((size_t)at.page * 2 * kv.nkv + (h - a.nq)) * kv.pt * DH + (size_t)c * kv.pt + off;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        v[(size_t)e * kv.pt] = f32_to_bf16(lo[u][e]);
+        v[(size_t)(DH / 2 + e) * kv.pt] = f32_to_bf16(hi[u][e]);
+      }
+      break;
+    }
     const float* gain = h < a.nq ? a.q_gain : a.k_gain;
     if (gain != nullptr) {
-      float ss = (lo.x * lo.x + lo.y * lo.y) + (lo.z * lo.z + lo.w * lo.w) + (hi.x * hi.x + hi.y * hi.y) + (hi.z * hi.z + hi.w * hi.w);
+      float ss = 0.f;
+#pragma unroll
+      for (int e = 0; e < N; ++e) ss += lo[u][e] * lo[u][e] + hi[u][e] * hi[u][e];
 #pragma unroll
       for (int o = 1; o < LPR; o *= 2) ss += __shfl_xor(ss, o);
       const float r = 1.0f / sqrtf(ss * (1.0f / DH) + a.eps);
-      const float4 gl = load4(gain + c), gh = load4(gain + DH / 2 + c);
-      lo = make_float4(lo.x * r * gl.x, lo.y * r * gl.y, lo.z * r * gl.z, lo.w * r * gl.w);
-      hi = make_float4(hi.x * r * gh.x, hi.y * r * gh.y, hi.z * r * gh.z, hi.w * r * gh.w);
+#pragma unroll
+      for (int e = 0; e < N; ++e) { lo[u][e] *= r * gain[c + e]; hi[u][e] *= r * gain[DH / 2 + c + e]; }
     }
     if (a.rope != nullptr) {
-      const float* t = a.rope + ((size_t)(kv.prefix_len + at.pos) * (DH / 2) + c) * 2;       // (cos, sin) of the four pairs
-      const float4 t0 = load4(t), t1 = load4(t + 4);
-      const float4 u = lo, w = hi;
-      lo = make_float4(u.x * t0.x - w.x * t0.y, u.y * t0.z - w.y * t0.w, u.z * t1.x - w.z * t1.y, u.w * t1.z - w.w * t1.w);
-      hi = make_float4(w.x * t0.x + u.x * t0.y, w.y * t0.z + u.y * t0.w, w.z * t1.x + u.z * t1.y, w.w * t1.z + u.w * t1.w);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float x = lo[u][e], y = hi[u][e];
+        lo[u][e] = x * cs[e] - y * sn[e];
+        hi[u][e] = y * cs[e] + x * sn[e];
+      }
     }
     if (h < a.nq) {
-      T* q = static_cast<T*>(a.q) + (size_t)i * a.ld_q + (size_t)h * DH;
-      store4(q + c, lo);
-      store4(q + DH / 2 + c, hi);
+      T* q = static_cast<T*>(a.q) + (size_t)i * a.ld_q + (size_t)h * DH + c;
+      store_piece(q, lo[u]);
+      store_piece(q + DH / 2, hi[u]);
     } else if (at.page >= 0) {
-      bf16_t* k = kv.pages + (((size_t)at.page * 2 * kv.nkv + (h - a.nq)) * kv.pt + off) * DH;
-      store4(k + c, lo);
-      store4(k + DH / 2 + c, hi);
+      bf16_t* k = kv.pages + (((size_t)at.page * 2 * kv.nkv + (h - a.nq)) * kv.pt + off) * DH + c;
+      store_piece(k, lo[u]);
+      store_piece(k + DH / 2, hi[u]);
     }
-  } else if (at.page >= 0) {
-    bf16_t* v = kv.pages + ((size_t)at.page * 2 * kv.nkv + (h - a.nq)) * kv.pt * DH + off;
-    const float e[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+  }
+}
+
+// Values of 64 rows of one head, into blocks [channel][position]: rows G of which are a run of consecutive positions that starts at a multiple of G
+// are written G positions at a time (a run belongs to the workgroup of its first row, which reads up to G - 1 rows of the next), others alone.
+constexpr int APPEND_RV = 64;        // rows of a workgroup
+template <int DH> struct ValueTile {
+  bf16_t v[APPEND_RV + 8][DH + 2];
+  int seq[APPEND_RV + 16], pos[APPEND_RV + 16], page[APPEND_RV + 16];      // from 8 rows in front on
+  unsigned char run[APPEND_RV + 8];                                        // a run starts here (from 8 rows in front on)
+  int n_run, n_one;
+  unsigned char runs[APPEND_RV], ones[APPEND_RV];                          // rows of this workgroup: first of a run, in none
+};
+template <int DH, typename T, int G>
+__device__ __forceinline__ void append_values(const AppendArgs& a, const int row_block, const int head, ValueTile<DH>& s) {
+  constexpr int rv = APPEND_RV, N = append_piece<T, 4>, LPR = DH / N;
+  const SharedKv& kv = a.kv;
+  const int r0 = row_block * rv, t = threadIdx.x;
+  const T* x = static_cast<const T*>(a.qkv) + (size_t)(a.nq + kv.nkv + head) * DH;
+  if (t < rv + 16) {
+    const int i = r0 - 8 + t;
+    const RowPlace p = i >= 0 ? row_place(a, i) : RowPlace{-1, -1, -1};
+    s.seq[t] = p.seq; s.pos[t] = p.pos; s.page[t] = p.page;
+  }
+  if (t == 0) { s.n_run = 0; s.n_one = 0; }
+  for (int i = t; i < (rv + G - 1) * LPR; i += 256) {
+    const int r = i / LPR, c = i % LPR * N;
+    if (r0 + r >= a.rows) break;
+    float v[N];
+    load_piece(x + (size_t)(r0 + r) * a.ld + c, v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[(size_t)(c + (j < 4 ? j : DH / 2 + j - 4)) * kv.pt] = f32_to_bf16(e[j]);
+    for (int e = 0; e < N; e += 2) *reinterpret_cast<uint32_t*>(&s.v[r][c + e]) = pack_bf16(v[e], v[e + 1]);
+  }
+  __syncthreads();
+  if (t < rv + 8) {                                             // (pages are multiples of four positions, of G where G is 8)
+    bool run = s.page[t] >= 0 && (s.pos[t] & (G - 1)) == 0 && t + G <= rv + 16;
+#pragma unroll
+    for (int j = 1; j < G; ++j) run = run && s.seq[t + j] == s.seq[t] && s.pos[t + j] == s.pos[t] + j;
+    s.run[t] = run;
+  }
+  __syncthreads();
+  if (t < rv) {
+    const int u = t + 8, first = u - (s.pos[u] & (G - 1));
+    if (s.run[u]) s.runs[atomicAdd(&s.n_run, 1)] = (unsigned char)t;
+    else if (s.page[u] >= 0 && !(s.run[first] && s.seq[first] == s.seq[u] && s.pos[first] + (u - first) == s.pos[u])) s.ones[atomicAdd(&s.n_one, 1)] = (unsigned char)t;
+  }
+  __syncthreads();
+  auto place = [&](const int r, const int ch) {
+    const int u = r + 8, off = s.pos[u] - page_of(kv, s.pos[u]) * kv.pt;
+    return kv.pages + ((size_t)s.page[u] * 2 * kv.nkv + kv.nkv + head) * kv.pt * DH + (size_t)ch * kv.pt + off;
+  };
+  for (int i = t; i < (s.n_run + 1) / 2 * 2 * DH; i += 256) {   // (two runs side by side: neighbours in a page, mostly)
+    const int k = (i & 1) + i / (2 * DH) * 2, ch = (i >> 1) % DH;
+    if (k >= s.n_run) continue;
+    const int r = s.runs[k];
+    uint32_t w[G / 2];
+#pragma unroll
+    for (int j = 0; j < G / 2; ++j) w[j] = s.v[r + 2 * j][ch] | ((uint32_t)s.v[r + 2 * j + 1][ch] << 16);
+    if constexpr (G == 8) *reinterpret_cast<u32x4*>(place(r, ch)) = u32x4{w[0], w[1], w[2], w[3]};
+    else *reinterpret_cast<uint2*>(place(r, ch)) = make_uint2(w[0], w[1]);
+  }
+  for (int i = t; i < s.n_one * DH; i += 256) *place(s.ones[i / DH], i % DH) = s.v[s.ones[i / DH]][i % DH];
+}
+
+// Workgroups of queries and keys first (HB heads of a row block side by side), then those of the values (HB == 1: none).
+template <int DH, typename T, int HB, int G>
+__global__ __launch_bounds__(256) void k_append(AppendArgs a, int n_heads_wgs, int head_groups, int value_blocks) {
+  int b = blockIdx.x;
+  if (HB == 1 || b < n_heads_wgs) {
+    append_heads<DH, T, HB>(a, b / head_groups, b % head_groups * HB);
+  } else if constexpr (HB > 1) {
+    __shared__ ValueTile<DH> s;
+    b -= n_heads_wgs;
+    append_values<DH, T, G>(a, b % value_blocks, b / value_blocks, s);
   }
 }
 
@@ -1049,19 +1171,21 @@ __global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
 
 // Sequence b of a group goes on from sequence parents[b].  Pages that are full are shared by reference; of the one being filled
 // the first child takes its parent's, further children get those of sequences without a child, with the contents copied.
-__global__ __launch_bounds__(256) void k_beam_reorder(BeamReorderArgs a, int copy_wgs) {
-  __shared__ int s_par[64], s_dst[64], s_src[64];
-  const int nb = a.n_beams, t = threadIdx.x;
-  const int unit = blockIdx.x, g = blockIdx.y;
+// Workgroups: `pieces` of every copied page of every layer (a sequence that needs no copy ends at once), then one for the group's tables.
+// Bound by the copies: 16 bytes a lane, four at a time.
+__global__ __launch_bounds__(256) void k_beam_reorder(BeamReorderArgs a, int pieces) {
+  __shared__ int s_par[64], s_dst[64], s_src[64], s_of[64], s_n;
+  const int nb = a.n_beams, t = threadIdx.x, g = blockIdx.y;
   const int32_t* old = a.tables + (size_t)g * nb * a.table_ld;
   if (t < 64) {
     int p = t < nb ? a.parents[(size_t)g * nb + t] : -1;
     if (t < nb && (unsigned)p >= (unsigned)nb) p = t;
     s_par[t] = p;
+    const int mine = t < nb && a.live ? old[(size_t)t * a.table_ld + a.full] : 0;     // the page being filled
     // (one wavefront: every lane sees all parents)
     bool further = false, childless = t < nb;
     for (int j = 0; j < nb; ++j) {
-      const int pj = __shfl(p, j);
+      const int pj = __builtin_amdgcn_readlane(p, j);
       further |= j < t && pj == p;
       childless &= pj != t;
     }
@@ -1070,19 +1194,31 @@ __global__ __launch_bounds__(256) void k_beam_reorder(BeamReorderArgs a, int cop
     const int rank = __popcll(fm & ((1ull << t) - 1));
     unsigned long long rest = em;                               // the rank-th sequence without a child
     for (int j = 0; j < rank; ++j) rest &= rest - 1;
-    const int own = t < nb && a.live ? old[(size_t)(further ? __ffsll(rest) - 1 : p) * a.table_ld + a.full] : 0;
-    s_dst[t] = own;
-    s_src[t] = further && a.live ? old[(size_t)p * a.table_ld + a.full] : -1;
+    const int src = __shfl(mine, p < 0 ? 0 : p), dst = __shfl(mine, further ? __ffsll(rest) - 1 : (p < 0 ? 0 : p));   // (all lanes active)
+    s_dst[t] = dst;
+    s_src[t] = src;
+    if (further) s_of[rank] = t;
+    if (t == 0) s_n = __popcll(fm);
   }
   __syncthreads();
-  if (unit < copy_wgs) {                                        // a layer of the pages to be copied
-    bf16_t* pages = a.pages + (size_t)unit * a.layer_stride;
-    for (int b = 0; b < nb; ++b) {
-      const int src = s_src[b], dst = s_dst[b];
-      if ((unsigned)src >= (unsigned)a.n_pages || (unsigned)dst >= (unsigned)a.n_pages) continue;
-      const u32x4* from = reinterpret_cast<const u32x4*>(pages + (size_t)src * a.page_elems);
-      u32x4* to = reinterpret_cast<u32x4*>(pages + (size_t)dst * a.page_elems);
-      for (int64_t i = t; i < a.page_elems / 8; i += 256) to[i] = from[i];
+  const int unit = blockIdx.x, n_units = (int)gridDim.x - 1;
+  if (unit < n_units) {
+    // unit = (layer, copied page, piece)
+    const int per_layer = (nb - 1) * pieces;                    // (at most n_beams - 1 pages are copied)
+    const int layer = unit / per_layer, k = unit % per_layer / pieces, piece = unit % pieces;
+    if (k >= s_n) return;
+    const int b = s_of[k], src = s_src[b], dst = s_dst[b];
+    if ((unsigned)src >= (unsigned)a.n_pages || (unsigned)dst >= (unsigned)a.n_pages) return;
+    bf16_t* pages = a.pages + (size_t)layer * a.layer_stride;
+    const u32x4* from = reinterpret_cast<const u32x4*>(pages + (size_t)src * a.page_elems);
+    u32x4* to = reinterpret_cast<u32x4*>(pages + (size_t)dst * a.page_elems);
+    const int64_t n = a.page_elems / 8, share = (n + pieces - 1) / pieces, end = min(n, share * (piece + 1));
+    for (int64_t i = share * piece + t; i < end; i += 1024) {
+      u32x4 x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) if (i + 256 * u < end) x[u] = from[i + 256 * u];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) if (i + 256 * u < end) to[i + 256 * u] = x[u];
     }
   } else {                                                      // the tables
     for (int i = t; i < nb * a.table_ld; i += 256) {
@@ -1102,17 +1238,27 @@ __global__ __launch_bounds__(256) void k_beam_reorder(BeamReorderArgs a, int cop
 // launches
 // ---------------------------------------------------------------------------------------------
 
-hipError_t launch_append(const AppendArgs& a, bool fp32, hipStream_t s) {
-  const int rpw = 256 / (a.kv.dh / 8);
-  const dim3 grid((unsigned)((a.rows + rpw - 1) / rpw), (unsigned)(a.nq + 2 * a.kv.nkv));
-  if (a.kv.dh == 128) {
-    if (fp32) hipLaunchKernelGGL((k_append<128, float>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((k_append<128, bf16_t>), grid, dim3(256), 0, s, a);
+// Calls whose rows can be runs (several tokens of a sequence) and whose values are worth 128 workgroups take four heads a workgroup and value
+// tiles: 5999 rows of 40 heads of their own 86 us against 150 with a head a workgroup and values written one by one; 192 rows of one token
+// 5.9 against 6.5, four rows 2.8 against 3.5 the other way round.
+template <int DH, typename T>
+static hipError_t launch_append_of(const AppendArgs& a, hipStream_t s) {
+  const int value_blocks = (a.rows + APPEND_RV - 1) / APPEND_RV;
+  auto row_blocks = [&](int piece) { const int rpw = 256 / (DH / 2 / piece); return (a.rows + rpw - 1) / rpw; };
+  if ((a.seq != nullptr || a.n_tok >= 4) && (long)value_blocks * a.kv.nkv >= 128) {
+    const int groups = (a.nq + a.kv.nkv + 3) / 4, n = row_blocks(append_piece<T, 4>) * groups;
+    const dim3 grid((unsigned)(n + value_blocks * a.kv.nkv));
+    if ((a.kv.pt & 7) == 0) hipLaunchKernelGGL((k_append<DH, T, 4, 8>), grid, dim3(256), 0, s, a, n, groups, value_blocks);
+    else hipLaunchKernelGGL((k_append<DH, T, 4, 4>), grid, dim3(256), 0, s, a, n, groups, value_blocks);
   } else {
-    if (fp32) hipLaunchKernelGGL((k_append<64, float>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((k_append<64, bf16_t>), grid, dim3(256), 0, s, a);
+    const int groups = a.nq + 2 * a.kv.nkv, n = row_blocks(append_piece<T, 1>) * groups;
+    hipLaunchKernelGGL((k_append<DH, T, 1, 8>), dim3((unsigned)n), dim3(256), 0, s, a, n, groups, 0);
   }
   return hipGetLastError();
+}
+hipError_t launch_append(const AppendArgs& a, bool fp32, hipStream_t s) {
+  if (a.kv.dh == 128) return fp32 ? launch_append_of<128, float>(a, s) : launch_append_of<128, bf16_t>(a, s);
+  return fp32 ? launch_append_of<64, float>(a, s) : launch_append_of<64, bf16_t>(a, s);
 }
 
 // Which rows share a workgroup, and how the positions are cut into ranges.  Up to 32 rows a K / V head (or a sequence) has: workgroups of that
@@ -1213,8 +1359,10 @@ hipError_t launch_beam_select(const BeamSelectArgs& a, bool fp32, hipStream_t s)
 }
 
 hipError_t launch_beam_reorder(const BeamReorderArgs& a, hipStream_t s) {
-  const int copies = a.live ? a.n_layers : 0;
-  hipLaunchKernelGGL(k_beam_reorder, dim3((unsigned)(copies + 1), (unsigned)a.n_groups), dim3(256), 0, s, a, copies);
+  // pieces of 64 KiB and more: sixteen loads a lane
+  const int pieces = (int)((a.page_elems * 2 + (64 << 10) - 1) >> 16);
+  const long units = a.live ? (long)a.n_layers * (a.n_beams - 1) * pieces : 0;
+  hipLaunchKernelGGL(k_beam_reorder, dim3((unsigned)(units + 1), (unsigned)a.n_groups), dim3(256), 0, s, a, pieces);
   return hipGetLastError();
 }
 
