@@ -538,6 +538,20 @@ int disco_beam_reorder(void* dev_pages, int n_layers, int64_t layer_stride, int 
                        int32_t* dev_tables_out, int table_ld, const int32_t* dev_parents, int n_groups, int n_beams, int len,
                        int page_tokens, disco_stream s);
 
+/* One decoding step of a model for n_seqs sequences (1 .. DISCO_MAX_BLOCK) behind the prompt that kv_prompt holds: feeds token
+ * dev_tokens[s] of every sequence at position kv_prompt->len + len - 1, appends its keys and values to the sequence's own pages in every layer and
+ * writes its fp32 logits to dev_logits [n_seqs][vocab].  The arithmetic is that of disco_verify (fp32-grade activations, bf16 cache).
+ * seqs: the sequences' pages of layer 0 (layer l at dev_pages + l * layer_stride elements), tables and lengths; page_tokens, n_kv_heads and d_head
+ * are the cache's, the fields of the prompt are not looked at.  len: the sequences' own length with this token, the value of every entry of
+ * dev_lens, at most table_ld * page_tokens (DISCO_ECAP).  The RMSNorm family takes the rotary table of kv_prompt, whose capacity has to reach
+ * len(prompt) + table_ld * page_tokens (DISCO_ECAP).  kv_prompt's length and entries are not changed.
+ * dev_ws: disco_step_workspace_bytes(m, kv_prompt, seqs) bytes, 256-byte aligned, initialised once by disco_workspace_init with max_block
+ * DISCO_MAX_BLOCK and max_ctx 0; a workspace for a longer prompt need not do for a shorter one (the bytes are checked).  No launch of it
+ * waits for another workgroup: steps may run on several streams at once, and replayed in graphs, with workspaces of their own.             */
+size_t disco_step_workspace_bytes(const disco_model* m, const disco_kv* kv_prompt, const disco_shared_kv* seqs);
+int disco_step(const disco_model* m, disco_kv* kv_prompt, const disco_shared_kv* seqs, int64_t layer_stride, int len,
+               const int32_t* dev_tokens, float* dev_logits, void* dev_ws, size_t ws_bytes, disco_stream s);
+
 /* ---- launch structure ------------------------------------------------------------------------------ */
 
 /* How a forward is cut into launches.  Process-wide; returns the previous mode, or DISCO_EINVAL.  Not to be

@@ -147,6 +147,9 @@ _SIGNATURES = {
     "disco_beam_select_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int, C.c_int]),
     "disco_beam_select": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_int,
                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "disco_step_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_void_p, C.POINTER(SharedKVDesc)]),
+    "disco_step": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(SharedKVDesc), C.c_int64, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                             C.c_void_p]),
     "disco_beam_reorder": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_int, C.c_int64, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int,
                                      C.c_int, C.c_int, C.c_int, C.c_void_p]),
     "disco_clf_examples": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
@@ -499,6 +502,54 @@ def disco_beam_reorder(pages, tables, parents, tables_out, n_groups: int, n_beam
                                     page_tokens, _raw_stream(dev, stream)))
 
 
+class Sequences:
+    """Own pages (of every layer), tables and lengths of n sequences that continue the prompt in a DiscoKV: room for `capacity` positions each.
+
+    pages: bf16 [layers, pages, 2, K / V heads, page_tokens * d_head]; tables: two, for disco_beam_reorder to go from one to the other."""
+
+    def __init__(self, model: "DiscoModel", n: int, capacity: int, page_tokens: int = 16):
+        s, dev = model.shape, model.device
+        self.n, self.page_tokens, cols = n, page_tokens, -(-capacity // page_tokens)
+        self.capacity = cols * page_tokens
+        self.pages = torch.empty(s.n_layers, n * cols, 2, s.n_kv_heads, page_tokens * s.d_head, dtype=torch.bfloat16, device=dev)
+        self.all_lens = torch.arange(1, self.capacity + 1, dtype=torch.int32, device=dev)[:, None].repeat(1, n).contiguous()
+        self.tables = [torch.arange(n * cols, dtype=torch.int32, device=dev).view(n, cols) for _ in range(2)]
+        self._kv = [SharedKV(self.pages[0], t, self.all_lens[0], page_tokens, s.n_kv_heads, s.d_head) for t in self.tables]
+        self.cur, self.len = 0, 0
+
+    def reset(self):
+        """Empty again; every table names pages of its own."""
+        t = self.tables[0]
+        t.copy_(torch.arange(t.numel(), dtype=torch.int32, device=t.device).view_as(t))
+        self.cur = self.len = 0
+
+    @property
+    def kv(self) -> SharedKV:
+        kv = self._kv[self.cur]
+        kv.c.dev_lens = self.all_lens.data_ptr() + 4 * self.n * max(self.len - 1, 0)
+        return kv
+
+
+def disco_step(model, kv_prompt, seqs: Sequences, tokens, logits, ws, stream=None):
+    """Feeds one token of every sequence; seqs.len grows by one."""
+    dev, vocab = _device(), model.shape.vocab
+    seqs.len += 1
+    try:
+        _check(lib().disco_step(model.handle, kv_prompt.handle, seqs.kv.ref, seqs.pages.stride(0), seqs.len,
+                                _tensor(tokens, "tokens", dev, torch.int32, seqs.n), _tensor(logits, "logits", dev, torch.float32, seqs.n * vocab),
+                                _ptr(ws.buf), ws.nbytes, _raw_stream(dev, stream)))
+    except DiscoError:
+        seqs.len -= 1
+        raise
+
+
+def disco_step_reorder(seqs: Sequences, parents, n_groups: int = 1, stream=None):
+    """disco_beam_reorder of the sequences, in n_groups groups."""
+    disco_beam_reorder(seqs.pages, seqs.tables[seqs.cur], parents, seqs.tables[1 - seqs.cur], n_groups, seqs.n // n_groups, seqs.len,
+                       seqs.page_tokens, stream)
+    seqs.cur = 1 - seqs.cur
+
+
 TRAIN_MAX_N = 2560
 PREFILL_MAX = 8192
 
@@ -655,6 +706,15 @@ class DiscoModel:
         _check(lib().disco_workspace_init(self.handle, ws.buf.data_ptr(), n, MAX_BLOCK, max_ctx, _stream()))
         return ws
 
+    def step_workspace(self, kv_prompt: "DiscoKV", seqs: "Sequences") -> "Workspace":
+        """Workspace of disco_step for the prompt that kv_prompt holds now."""
+        n = lib().disco_step_workspace_bytes(self.handle, kv_prompt.handle, seqs.kv.ref)
+        if n == 0:
+            raise DiscoError(EINVAL, last_error())
+        ws = Workspace(n, self.device)
+        _check(lib().disco_workspace_init(self.handle, ws.buf.data_ptr(), n, MAX_BLOCK, 0, _stream()))
+        return ws
+
     def close(self):
         if self.handle:
             lib().disco_model_destroy(self.handle)
@@ -676,6 +736,7 @@ class Workspace:
 class DiscoKV:
     def __init__(self, model: DiscoModel, capacity: int, page_tokens: int = 16, page_order=None):
         self.model = model
+        self.capacity = -(-capacity // page_tokens) * page_tokens
         nbytes = lib().disco_kv_bytes(model.handle, capacity, page_tokens)
         self.buf = torch.empty(nbytes, dtype=torch.uint8, device=model.device)
         order = None

@@ -71,29 +71,9 @@ template <bool COH> __device__ __forceinline__ void st_f1(float* p, float v) {
   if (COH) __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   else *p = v;
 }
-template <bool COH> __device__ __forceinline__ void st_u2(bf16_t* p, uint2 v) {
-  if (COH) __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), (unsigned long long)v.x | ((unsigned long long)v.y << 32), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  else *reinterpret_cast<uint2*>(p) = v;
-}
 template <bool COH> __device__ __forceinline__ void st_h1(bf16_t* p, bf16_t v) {
   if (COH) __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   else *p = v;
-}
-
-// Store 4 consecutive-k activations of token m into the packed panels as bf16 hi/lo (LO false: the lo panel has no reader).
-template <bool COH = false, bool LO = true>
-__device__ __forceinline__ void xpack_put4(bf16_t* X, int KT, int M, int m, int k, HiLo x0, HiLo x1) {
-  const int kt = k >> 5, grp = (k & 31) >> 3, e = k & 7;
-  const size_t base = ((size_t)kt * 64 + grp * 16) * 8 + e;
-  size_t off_hi, off_lo;
-  if (M <= 8) { off_hi = base + (size_t)m * 8; off_lo = base + (size_t)(m + 8) * 8; }
-  else { off_hi = base + (size_t)m * 8; off_lo = (size_t)KT * 512 + base + (size_t)m * 8; }
-  st_u2<COH>(X + off_hi, make_uint2(x0.hi, x1.hi));
-  if (LO) st_u2<COH>(X + off_lo, make_uint2(x0.lo, x1.lo));
-}
-template <bool COH = false, bool LO = true>
-__device__ __forceinline__ void xpack_store4(bf16_t* X, int KT, int M, int m, int k, const float* v) {
-  xpack_put4<COH, LO>(X, KT, M, m, k, split_bf16(v[0], v[1]), split_bf16(v[2], v[3]));
 }
 
 // The products a * ga and b * gb as bf16 hi + lo.  EXACT: lo is what hi leaves of the exact product, else of the product rounded to

@@ -42,6 +42,7 @@ struct SharedAttnArgs {
   SharedKv kv;
   const void* q; int64_t ld_q; int n_tok, nq; float scale;
   void* out; int64_t ld_out; float* lse;
+  bf16_t* panels;                    // fp32, up to sixteen rows: the result goes here instead of `out`, as the next matrix' input
   float* part; float2* ml;           // [part][kv head][row][channel] and their (maximum in log2 units, sum)
   SharedAttnPlan plan;
 };
@@ -65,5 +66,12 @@ struct BeamReorderArgs {
   int n_groups, n_beams, full, live;
 };
 hipError_t launch_beam_reorder(const BeamReorderArgs& a, hipStream_t s);
+
+struct BeamEmbedArgs {
+  const int32_t* tokens; int rows, vocab, d;
+  const bf16_t* tok_emb; int64_t tok_stride; const bf16_t* pos_row;   // pos_row: the position's row of the position table, or nullptr
+  const float* gain; float* h; bf16_t* panels; float* ssq; float* sum; int n_slots;
+};
+hipError_t launch_beam_embed(const BeamEmbedArgs& a, hipStream_t s);
 
 }  // namespace disco

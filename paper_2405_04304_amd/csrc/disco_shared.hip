@@ -563,6 +563,12 @@ struct AttnRows {
   }
 };
 
+// Four channels of a row as the next matrix' input (panels of up to sixteen rows).
+__device__ __forceinline__ void put_panels(const SharedAttnArgs& a, const int row, const int k, const float4 o) {
+  const float v[4] = {o.x, o.y, o.z, o.w};
+  xpack_store4(a.panels, (a.nq * a.kv.dh) >> 5, a.kv.n_seqs * a.n_tok, row, k, v);
+}
+
 // A row's result: to the output, or as this range's part.
 template <int DH, bool F32>
 struct AttnPut {
@@ -578,6 +584,10 @@ struct AttnPut {
     }
     const float inv = l == 0.f ? 0.f : 1.0f / l;
     o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    if (F32 && a.panels != nullptr) {
+      put_panels(a, r / grp, (it.kvh * grp + r % grp) * DH + c, o);
+      return;
+    }
     const size_t at = (size_t)(r / grp) * a.ld_out + (size_t)(it.kvh * grp + r % grp) * DH + c;
     if constexpr (F32) store4(static_cast<float*>(a.out) + at, o);
     else store4(static_cast<bf16_t*>(a.out) + at, o);
@@ -858,7 +868,8 @@ __global__ __launch_bounds__(256) void k_shared_merge(SharedAttnArgs a) {
   const int kvh = (int)(i / head_rows), row = (int)(i % head_rows), tr = row / grp, head = kvh * grp + row % grp;
   const float inv = l == 0.f ? 0.f : 1.0f / l;
   o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-  if constexpr (F32) store4(static_cast<float*>(a.out) + (size_t)tr * a.ld_out + (size_t)head * DH + me * 4, o);
+  if (F32 && a.panels != nullptr) put_panels(a, tr, head * DH + me * 4, o);
+  else if constexpr (F32) store4(static_cast<float*>(a.out) + (size_t)tr * a.ld_out + (size_t)head * DH + me * 4, o);
   else store4(static_cast<bf16_t*>(a.out) + (size_t)tr * a.ld_out + (size_t)head * DH + me * 4, o);
   if (me == 0 && a.lse != nullptr) a.lse[(size_t)tr * a.nq + head] = l == 0.f ? -INFINITY : (m + __log2f(l)) * LN2;
 }
@@ -1232,7 +1243,43 @@ __global__ __launch_bounds__(256) void k_beam_reorder(BeamReorderArgs a, int pie
   }
 }
 
+// ---------------------------------------------------------------------------------------------
+// embedding of a step
+// ---------------------------------------------------------------------------------------------
+
+// Token of every sequence, all at one position: residual row, its sum of squares (and sum, for a LayerNorm) in the first slot, and the panels of
+// gain * row.  A workgroup a row.
+__global__ __launch_bounds__(256) void k_beam_embed(BeamEmbedArgs a) {
+  __shared__ float red[2][4];
+  const int m = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6;
+  const int tok = min(max(a.tokens[m], 0), a.vocab - 1);
+  const bf16_t* e = a.tok_emb + (size_t)tok * a.tok_stride;
+  float ss = 0.f, sx = 0.f;
+  for (int k = t * 4; k < a.d; k += 1024) {
+    float4 v = load4(e + k);
+    if (a.pos_row != nullptr) { const float4 p = load4(a.pos_row + k); v = make_float4(v.x + p.x, v.y + p.y, v.z + p.z, v.w + p.w); }
+    store4(a.h + (size_t)m * a.d + k, v);
+    ss += (v.x * v.x + v.y * v.y) + (v.z * v.z + v.w * v.w);
+    sx += (v.x + v.y) + (v.z + v.w);
+    const float4 g = load4(a.gain + k);
+    const float o[4] = {v.x * g.x, v.y * g.y, v.z * g.z, v.w * g.w};
+    xpack_store4(a.panels, a.d >> 5, a.rows, m, k, o);
+  }
+  ss = wave_sum(ss); sx = wave_sum(sx);
+  if (lane == 0) { red[0][w] = ss; red[1][w] = sx; }
+  __syncthreads();
+  for (int i = t; i < a.n_slots; i += 256) {
+    a.ssq[i * 16 + m] = i == 0 ? (red[0][0] + red[0][1]) + (red[0][2] + red[0][3]) : 0.f;
+    if (a.sum != nullptr) a.sum[i * 16 + m] = i == 0 ? (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]) : 0.f;
+  }
+}
+
 }  // namespace
+
+hipError_t launch_beam_embed(const BeamEmbedArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(k_beam_embed, dim3((unsigned)a.rows), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
 
 // ---------------------------------------------------------------------------------------------
 // launches

@@ -223,3 +223,126 @@ int disco_beam_reorder(void* dev_pages, int n_layers, int64_t layer_stride, int 
   HIP_TRY(launch_beam_reorder(a, static_cast<hipStream_t>(s)), "reorder launch");
   return DISCO_OK;
 }
+
+// ---- a decoding step of a model for several sequences ------------------------------------------------
+
+namespace {
+
+// Workspace of a step: an ordinary one first (max_ctx 0), then the rows and parts of the operators above.
+struct StepWs { Ws base; float* qkv; float* q; void* attn; size_t attn_bytes, total; };
+StepWs carve_step(const disco_model* m, const disco_shared_kv& k, void* ws) {
+  StepWs w;
+  w.base = carve(m, DISCO_MAX_BLOCK, 0, ws);
+  char* p = static_cast<char*>(ws);
+  size_t off = w.base.total;
+  auto take = [&](size_t bytes) { void* r = p ? p + off : nullptr; off += round_up(bytes, 256); return r; };
+  w.qkv = static_cast<float*>(take(sizeof(float) * 16 * m->d_qkv));
+  w.q = static_cast<float*>(take(sizeof(float) * 16 * m->d_q));
+  w.attn_bytes = disco_attn_shared_bytes(&k, 1, m->d.n_heads, 0);
+  w.attn = take(w.attn_bytes);
+  w.total = off;
+  return w;
+}
+
+// The caller's sequences behind the prompt that kv holds, for layer l.
+int check_step(const disco_model* m, const disco_kv* kv, const disco_shared_kv* seqs, disco_shared_kv* out) {
+  if (!m || !kv || !seqs) return fail(DISCO_EINVAL, "null argument");
+  if (kv->model != m) return fail(DISCO_ESTATE, "KV cache belongs to another model");
+  *out = *seqs;
+  out->dev_prefix = kv->pages; out->dev_prefix_table = kv->dev_page_table; out->n_prefix_pages = kv->n_pages; out->prefix_len = kv->len;
+  if (seqs->n_kv_heads != m->d.n_kv_heads || seqs->d_head != m->d.d_head || seqs->page_tokens != kv->page_tokens)
+    return fail(DISCO_EINVAL, "the sequences' pages have another shape than the model's cache");
+  const int rc = check_shape(out);
+  if (rc) return rc;
+  if (seqs->n_seqs < 1 || seqs->n_seqs > DISCO_MAX_BLOCK) return fail(DISCO_EINVAL, "%d sequences outside [1, %d]", seqs->n_seqs, DISCO_MAX_BLOCK);
+  return DISCO_OK;
+}
+
+}  // namespace
+
+size_t disco_step_workspace_bytes(const disco_model* m, const disco_kv* kv_prompt, const disco_shared_kv* seqs) {
+  disco_shared_kv k;
+  return check_step(m, kv_prompt, seqs, &k) ? 0 : carve_step(m, k, nullptr).total;
+}
+
+int disco_step(const disco_model* m, disco_kv* kv_prompt, const disco_shared_kv* seqs, int64_t layer_stride, int len, const int32_t* dev_tokens,
+               float* dev_logits, void* dev_ws, size_t ws_bytes, disco_stream st) {
+  disco_shared_kv k;
+  int rc = check_step(m, kv_prompt, seqs, &k);
+  if (rc) return rc;
+  const disco_model_desc& d = m->d;
+  const int n = k.n_seqs, cap = k.table_ld * k.page_tokens, pos = k.prefix_len + len - 1, n_tiles = d.d_model / 16;
+  const bool fam_a = d.family == DISCO_FAMILY_A;
+  hipStream_t s = static_cast<hipStream_t>(st);
+  if (!dev_tokens || !dev_logits || !dev_ws || !k.dev_lens) return fail(DISCO_EINVAL, "null argument");
+  if ((rc = check_cache(&k, true))) return rc;
+  if (!aligned(dev_tokens, 4) || !aligned(dev_logits, 16) || !aligned(dev_ws, 256)) return fail(DISCO_EINVAL, "misaligned pointer");
+  if (len < 1 || len > cap) return fail(DISCO_ECAP, "%d own positions, tables hold %d", len, cap);
+  if (fam_a && pos >= d.max_pos) return fail(DISCO_ECAP, "position table of %d rows exceeded", d.max_pos);
+  if (!fam_a && kv_prompt->capacity < k.prefix_len + cap)
+    return fail(DISCO_ECAP, "the prompt's cache has a rotary table for %d positions, %d + %d needed", kv_prompt->capacity, k.prefix_len, cap);
+  const int64_t page_elems = (int64_t)2 * k.n_kv_heads * k.page_tokens * k.d_head;
+  if (layer_stride < 0 || layer_stride % 8 || (d.n_layers > 1 && layer_stride / page_elems < k.n_pages)) return fail(DISCO_EINVAL, "bad page pool");
+  const StepWs ws = carve_step(m, k, dev_ws);
+  if (ws_bytes < ws.total) return fail(DISCO_EINVAL, "workspace of %zu bytes, %zu needed", ws_bytes, ws.total);
+  if (kv_prompt->dev_rope && !kv_prompt->rope_ready) {
+    HIP_TRY(launch_rope_fill(kv_prompt->dev_rope, kv_prompt->capacity, d.d_head, d.rope_base, s), "rotary table launch");
+    kv_prompt->rope_ready = true;
+  }
+  const Ws& b = ws.base;
+  const int split_o = gemm_split_for(d.d_model, m->d_q / 32, n), split_dn = gemm_split_for(d.d_model, d.d_ff / 32, n);
+
+  // every norm is applied inside the matrix that reads the row, as in the forwards of one sequence
+  auto normed_input = [&](GemmArgs& g, const float* ln_vec, int n_rows) {
+    g.M = n; g.X = b.xn; g.KT = d.d_model / 32; g.planes = b.gpart; g.counters = b.gemm_counters; g.n_rows = n_rows;
+    g.ssq = b.ssq; g.n_ssq = n_tiles; g.d_in = d.d_model; g.eps = d.norm_eps;
+    if (fam_a) { g.sum = b.sum; g.wg = ln_vec; g.wb = ln_vec + n_rows; }
+  };
+  auto residual_update = [&](const void* w, const bf16_t* x, int kdim, int split, const float* next_gain, const char* what) -> int {
+    GemmArgs g{};
+    g.M = n; g.W = static_cast<const bf16_t*>(w); g.X = x; g.KT = kdim / 32; g.n_rows = d.d_model; g.h = b.h; g.ld_out = d.d_model; g.only_row = -1;
+    g.n_split = split; g.planes = b.gpart; g.counters = b.gemm_counters;
+    g.Xout = b.xn; g.KT_out = d.d_model / 32; g.gain = next_gain; g.ssq_out = b.ssq; g.n_ssq_out = n_tiles;
+    if (fam_a) g.sum_out = b.sum;
+    HIP_TRY(launch_gemm(g, EPI_PARTIAL, s), what);
+    return DISCO_OK;
+  };
+
+  BeamEmbedArgs e{};
+  e.tokens = dev_tokens; e.rows = n; e.vocab = d.vocab; e.d = d.d_model; e.tok_emb = static_cast<const bf16_t*>(m->w.tok_emb); e.tok_stride = m->w.tok_emb_stride;
+  e.pos_row = fam_a ? static_cast<const bf16_t*>(m->w.pos_emb) + (size_t)pos * d.d_model : nullptr;
+  e.gain = m->layers[0].norm1_g; e.h = b.h; e.panels = b.xn; e.ssq = b.ssq; e.sum = fam_a ? b.sum : nullptr; e.n_slots = n_tiles;
+  HIP_TRY(launch_beam_embed(e, s), "embedding launch");
+  AppendArgs ap{};
+  ap.qkv = ws.qkv; ap.ld = m->d_qkv; ap.rows = n; ap.nq = d.n_heads; ap.n_tok = 1; ap.rope = kv_prompt->dev_rope; ap.q = ws.q; ap.ld_q = m->d_q;
+  SharedAttnArgs at{};
+  at.plan = attn_plan(&k, true, 1, d.n_heads, 0);
+  if (!launchable(&k, at.plan)) return fail(DISCO_EINVAL, "more workgroups than a launch takes");
+  at.q = ws.q; at.ld_q = m->d_q; at.n_tok = 1; at.nq = d.n_heads; at.scale = 1.0f / sqrtf((float)d.d_head); at.panels = b.xattn;
+  at.part = static_cast<float*>(ws.attn); at.ml = reinterpret_cast<float2*>(at.part + (size_t)at.plan.parts * n * m->d_q);
+  for (int l = 0; l < d.n_layers; ++l) {
+    const disco_layer_weights& L = m->layers[l];
+    const float* next_g = l + 1 == d.n_layers ? m->w.normf_g : m->layers[l + 1].norm1_g;
+    const float* ln_l = fam_a ? b.ln_vec + b.ln_layer_stride * l : nullptr;
+    k.dev_prefix = kv_prompt->pages + (size_t)l * kv_prompt->layer_stride;
+    k.dev_pages = static_cast<bf16_t*>(seqs->dev_pages) + (size_t)l * layer_stride;
+    ap.kv = at.kv = device_view(k);
+    GemmArgs g{};
+    normed_input(g, ln_l, m->d_qkv);
+    g.W = static_cast<const bf16_t*>(L.wqkv); g.out = ws.qkv; g.ld_out = m->d_qkv; g.only_row = -1;
+    HIP_TRY(launch_gemm(g, EPI_STORE, s), "qkv launch");
+    HIP_TRY(launch_append(ap, true, s), "append launch");
+    HIP_TRY(launch_shared_attn(at, true, s), "attention launch");
+    if ((rc = residual_update(L.wo, b.xattn, m->d_q, split_o, L.norm2_g, "o-proj launch"))) return rc;
+    GemmArgs u{};
+    normed_input(u, fam_a ? ln_l + 2 * (size_t)m->d_qkv : nullptr, fam_a ? d.d_ff : 2 * d.d_ff);
+    u.W = static_cast<const bf16_t*>(L.w_in); u.grp = 1; u.Xout = b.xact; u.KT_out = d.d_ff / 32;
+    HIP_TRY(launch_gemm(u, fam_a ? EPI_GELU : EPI_SWIGLU, s), "mlp-in launch");
+    if ((rc = residual_update(L.w_out, b.xact, d.d_ff, split_dn, next_g, "mlp-out launch"))) return rc;
+  }
+  GemmArgs lm{};
+  normed_input(lm, fam_a ? b.ln_vec + b.ln_layer_stride * d.n_layers : nullptr, d.vocab);
+  lm.W = static_cast<const bf16_t*>(m->w.wlm); lm.out = dev_logits; lm.ld_out = d.vocab; lm.only_row = -1;
+  HIP_TRY(launch_gemm(lm, EPI_STORE, s), "lm-head launch");
+  return DISCO_OK;
+}

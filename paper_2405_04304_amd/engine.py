@@ -20,7 +20,7 @@ class SpecEngine:
                  max_ctx: int, page_tokens: int = 16, page_order_target=None, page_order_draft=None):
         self.target, self.draft, self.clf = target, draft, clf
         self.dev = target.device
-        self.max_ctx = max_ctx
+        self.max_ctx, self.page_tokens = max_ctx, page_tokens
         cap = max_ctx + B.MAX_BLOCK
         self.kv_t = B.DiscoKV(target, cap, page_tokens, page_order_target)
         self.ws_t = target.workspace(B.MAX_BLOCK, cap)
@@ -82,6 +82,55 @@ class SpecEngine:
             B.disco_verify(self.target, self.kv_t, self.tok_in, 1, self.argmax, None, self.ws_t)
             last = int(self.argmax[0].item())
             out.append(last)
+        return out
+
+    def beam_search(self, prompt: Sequence[int], n_beams: int, max_new: int, end_token: int = -1) -> List[Dict]:
+        """Beam search of the target: the n_beams sequences of up to max_new tokens with the largest sum of log probabilities that the search
+        keeps, best first, as {"tokens", "score"}.  A sequence ends with end_token (-1: none does).  The prompt's cache is read by all beams
+        and not changed; nothing comes back to the host before the end but, every eight tokens, whether all beams have ended."""
+        assert 1 <= n_beams <= B.MAX_BLOCK and max_new >= 1
+        self.reset()
+        self.prefill(prompt[:-1])
+        dev, vocab = self.dev, self.target.shape.vocab
+        need = self.kv_t.len + -(-max_new // self.page_tokens) * self.page_tokens
+        if need > self.kv_t.capacity:
+            raise ValueError(f"{need} positions in a cache of {self.kv_t.capacity}")
+        seqs = B.Sequences(self.target, n_beams, max_new, self.page_tokens)
+        ws = self.target.step_workspace(self.kv_t, seqs)
+        logits = torch.empty(n_beams, vocab, dtype=torch.float32, device=dev)
+        hist = torch.empty(2, max_new, n_beams, dtype=torch.int32, device=dev)      # tokens, parents
+        scores = torch.full((2, n_beams), float("-inf"), dtype=torch.float32, device=dev)
+        scores[0, 0] = 0.0                                                          # all beams start as one
+        done = torch.zeros(2, n_beams, dtype=torch.int32, device=dev)
+        select_ws = torch.empty(B.disco_beam_select_bytes(1, n_beams, vocab, n_beams), dtype=torch.uint8, device=dev)
+        tokens = torch.full((n_beams,), int(prompt[-1]), dtype=torch.int32, device=dev)
+        n = 0
+        while n < max_new:
+            B.disco_step(self.target, self.kv_t, seqs, tokens, logits, ws)
+            a, b = n & 1, 1 - (n & 1)
+            tokens = hist[0, n]
+            B.disco_beam_select(logits, scores[a], 1, n_beams, n_beams, tokens, hist[1, n], scores[b], select_ws,
+                                done=done[a] if end_token >= 0 else None, done_out=done[b], end_token=end_token)
+            n += 1
+            if n < max_new:
+                B.disco_step_reorder(seqs, hist[1, n - 1])
+                if end_token >= 0 and n % 8 == 0 and bool(done[b].all()):
+                    break
+        toks, pars, final = hist[0, :n].tolist(), hist[1, :n].tolist(), scores[n & 1].tolist()
+        out = []
+        for beam in range(n_beams):
+            seq, at = [], beam
+            for t in range(n - 1, -1, -1):
+                if at < 0:                                      # a place that no candidate filled
+                    break
+                seq.append(toks[t][at])
+                at = pars[t][at]
+            seq.reverse()
+            if at < 0 or len(seq) < n:
+                continue
+            if end_token >= 0 and end_token in seq:
+                seq = seq[:seq.index(end_token) + 1]
+            out.append({"tokens": seq, "score": final[beam]})
         return out
 
     # -- labelling run and classifier training (App. D.1, Sec. 4) ---------------------------------
