@@ -29,7 +29,7 @@ hipError_t launch_append(const AppendArgs& a, bool fp32, hipStream_t s);
 constexpr int ATTN_MAX_PARTS = 256;
 struct SharedAttnPlan {
   bool fused;                        // every workgroup walks the prompt before its sequence's own positions: one launch, one part
-  int few_rows;                      // rows (16 or 32) of a workgroup that is not one of 128
+  int few_rows, few_waves;           // rows (16 or 32) and wavefronts of a workgroup that is not one of 128 rows
   bool prefix_many, own_many;        // workgroups of 128 rows
   int prefix_tiles, prefix_splits, prefix_len;    // row tiles of a kv head, ranges, positions of a range
   int own_tiles, own_splits, own_len;

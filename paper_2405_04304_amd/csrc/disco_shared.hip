@@ -263,13 +263,15 @@ struct AttnItem {
   int first;                         // own positions: those below it are seen by every token of the call (prompt: end)
 };
 
-// A block of 32 positions in LDS, 16-byte chunks.  K: chunk c of the row in place m at m * DH / 8 + (c ^ m): a copy of 1 KiB is rows of four
+// A block of 32 positions in LDS, 16-byte chunks.  K: chunk c of the row in place m at m * DH / 8 + (c ^ k_swizzle(m)): a copy of 1 KiB is rows of four
 // consecutive positions each, and a fragment read (one chunk column of many rows) meets no bank twice.  Places: a lane's scores have to be those
 // of eight consecutive positions (see AttnRows), which are in places four apart from each other.  V: eight positions of a channel, half h of group g
-// of sixteen at (g * DH + channel) * 2 + (h ^ channel / 4): a copy takes consecutive bytes of a page of sixteen, a read is free of conflicts.
+// of sixteen at (g * DH + channel) * 2 + (h ^ channel / 16): a copy takes consecutive bytes of a page of sixteen, and a read meets no bank twice either (a
+// 16-byte read of a wavefront goes through LDS in four sets of lanes: 0-3, 12-15, 20-23 and 24-27 are the first).
 template <int DH> struct AttnBlock {
   static constexpr int CK = DH / 8, K_CHUNKS = 32 * CK, V_CHUNKS = 4 * DH, COPIES = DH / 16;     // copies (of K, of V) of a wavefront's width
 };
+template <int DH> __device__ __forceinline__ constexpr int k_swizzle(int m) { return DH == 128 ? m & 15 : (m >> 1) & 7; }
 // Which four positions (of a block's eight fours) are in the four places 4 j ..
 template <int RB> __device__ __forceinline__ constexpr int four_of(int j) {
   return RB == 32 ? (j & 4) | ((j & 1) << 1) | ((j & 2) >> 1) : ((j & 3) << 1) | (j >> 2);
@@ -330,7 +332,7 @@ struct BlockCopy {
         lds_dma_16(reinterpret_cast<const void*>(lane_value(k_addr, n + four_of<RB>(j))), at, lds + (uint32_t)j * 1024u);
       } else {                                 // eight, of two fours
         const uint64_t b0 = lane_value(k_addr, n + four_of<RB>(2 * j)), b1 = lane_value(k_addr, n + four_of<RB>(2 * j + 1));
-        const uint32_t at = (uint32_t)((lane >> 3) & 3) * (DH * 2) + (uint32_t)(((lane & 7) ^ (lane >> 3)) * 16);
+        const uint32_t at = (uint32_t)((lane >> 3) & 3) * (DH * 2) + (uint32_t)(((lane & 7) ^ (lane >> 4) ^ (4 * (j & 1))) * 16);
         lds_dma_16(reinterpret_cast<const void*>(((lane & 32) ? b1 : b0) + at), lds + (uint32_t)j * 1024u);
       }
     }
@@ -339,7 +341,7 @@ struct BlockCopy {
   template <int J0, int J1>
   __device__ __forceinline__ void copy_v(const int i, const uint32_t lds, u32x4* v) const {
     constexpr int PER_G = DH / 32;             // copies of sixteen positions
-    const int lane = threadIdx.x & 63, n = 8 * (i & 7), half = (lane ^ (lane >> 3)) & 1;
+    const int lane = threadIdx.x & 63, n = 8 * (i & 7), half = (lane ^ (lane >> 5)) & 1;
     const uint64_t row = (uint64_t)(uint32_t)((lane >> 1) * kv.pt * 2);
     if ((kv.pt & 7) == 0) {
       uint64_t b = 0;
@@ -371,7 +373,7 @@ template <int DH>
 __device__ __forceinline__ bool mend_values(const AttnItem& it, const int base, u32x4* vs, const int i0, const int step) {
   bool odd = false;
   for (int i = i0; i < AttnBlock<DH>::V_CHUNKS; i += step) {
-    const int ch = (i >> 1) % DH, half = (i ^ (ch >> 2)) & 1, at = base + 16 * (i / (2 * DH)) + 8 * half;
+    const int ch = (i >> 1) % DH, half = (i ^ (ch >> 4)) & 1, at = base + 16 * (i / (2 * DH)) + 8 * half;
     if (at + 8 <= it.first) continue;
     u32x4 v = vs[i];
     const int n = it.end - at, n_all = it.first - at;
@@ -461,7 +463,7 @@ struct AttnRows {
     Acc S[TILES];
     auto k_frag = [&](const int i) {
       const int place = i % TILES * RB + col;
-      return as_bf16x8(ks[place * CK + ((64 / RB * (i / TILES) + hf) ^ (place & (CK - 1)))]);
+      return as_bf16x8(ks[place * CK + ((64 / RB * (i / TILES) + hf) ^ k_swizzle<DH>(place & 31))]);
     };
     bf16x8 kk[AHEAD + 1];
 #pragma unroll
@@ -523,7 +525,7 @@ struct AttnRows {
     u32x4 vv[2][CB];
     auto v_frag = [&](const int s, const int c) {
       const int ch = RB * c + col, g = RB == 32 ? s : 2 * s + (hf >> 1), half = RB == 32 ? hf : hf & 1;
-      return vs[(g * DH + ch) * 2 + (half ^ ((col >> 2) & 1))];
+      return vs[(g * DH + ch) * 2 + (half ^ ((ch >> 4) & 1))];
     };
 #pragma unroll
     for (int c = 0; c < CB; ++c) vv[0][c] = v_frag(0, c);
@@ -665,7 +667,7 @@ __device__ __forceinline__ void attn_many(const SharedAttnArgs& a, const AttnIte
 template <int DH, int RB, int WT, bool F32> struct FewShape {
   typedef AttnBlock<DH> Bk;
   static constexpr int OLD = DH + 4;                            // a row put together in LDS
-  static constexpr size_t stage = (size_t)WT * (Bk::K_CHUNKS + Bk::V_CHUNKS) * 16, merge = (size_t)(WT * RB * (OLD + 2) + 4 * WT) * 4;
+  static constexpr size_t stage = (size_t)WT * (Bk::K_CHUNKS + Bk::V_CHUNKS) * 16, merge = WT == 1 ? 0 : (size_t)(WT * RB * (OLD + 2) + 4 * WT) * 4;
   static constexpr size_t lds = stage > merge ? stage : merge;
 };
 template <int DH, int RB, int WT, bool F32>
@@ -726,6 +728,17 @@ __device__ __forceinline__ void attn_few(const SharedAttnArgs& a, const AttnItem
   const float l_wave = x.row_sum();
   const AttnPut<DH, F32> put(a, it);
   constexpr int AV = AttnRows<DH, RB, F32>::AV, CB = AttnRows<DH, RB, F32>::CB;
+  if constexpr (WT == 1) {
+    if (col < it.rows) {
+      const float l = bad < x.see ? NAN : l_wave;
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int i = 0; i < AV; i += 4) put.row(r_mine, x.channel(c, i), make_float4(x.O[c][i], x.O[c][i + 1], x.O[c][i + 2], x.O[c][i + 3]), l);
+      if (x.hf == 0) put.stat(r_mine, x.m_run, l);
+    }
+    return;
+  }
   float* sm = reinterpret_cast<float*>(lds);                    // [WT][RB] maxima, sums, first bad positions, then rows
   float* sl = sm + WT * RB;
   int* sb = reinterpret_cast<int*>(sl + WT * RB);
@@ -1314,7 +1327,9 @@ hipError_t launch_append(const AppendArgs& a, bool fp32, hipStream_t s) {
 // two workgroups a compute unit (one where registers allow no more), but one where a range would then have no more than 512 positions: what is
 // gained is less than what the additional parts cost (4608 rows over 3001 positions: 28 us with one, 32 with two; 384 over 65537: 245 and 193).
 // A prompt and own positions that four wavefronts walk in two steps take one launch, every sequence reading the prompt by itself: 100 + 20
-// positions of 12 heads 7.9 us against 9.9, but 523 + 37 for four sequences 13.2 against 10.4.
+// positions of 12 heads 7.9 us against 9.9, but 523 + 37 for four sequences 13.2 against 10.4.  Such workgroups have four wavefronts where two fit
+// every compute unit, and all have one where they are more than four for each: 71 sequences of 40 heads, 3 positions: 30 us with one, 46 with two, 84
+// with four; 32 of 40 heads, 300 + 100 positions: 32 and 38 with one and two, but 8 of them with 2048 + 130: 25 and 20.
 SharedAttnPlan shared_attn_plan(int n_seqs, int n_tok, int nq, int nkv, int dh, bool fp32, int prefix_len, int max_len) {
   SharedAttnPlan p{};
   const long grp = nq / nkv, own_rows = n_tok * grp, rows = n_seqs * own_rows;
@@ -1348,6 +1363,8 @@ SharedAttnPlan shared_attn_plan(int n_seqs, int n_tok, int nq, int nkv, int dh, 
     }
     ranges(p.own_many, (long)p.own_tiles * nkv * n_seqs, max_len, &p.own_splits, &p.own_len);
   }
+  const long few = (p.own_many ? 0 : (long)n_seqs * nkv * p.own_splits) + (p.prefix_many ? 0 : (long)p.prefix_tiles * nkv * p.prefix_splits);
+  p.few_waves = few > 1024 ? 1 : (p.fused && few <= 512 ? 4 : 2);
   p.few_rows = (p.prefix_tiles > 0 && !p.prefix_many ? rows : own_rows) <= 16 ? 16 : 32;
   p.parts = p.prefix_splits + p.own_splits;
   if (p.parts > 1) p.bytes = (size_t)p.parts * rows * nkv * (dh * sizeof(float) + sizeof(float2));
@@ -1360,10 +1377,12 @@ static hipError_t launch_attn_all(const SharedAttnArgs& a, hipStream_t s) {
   const unsigned n_prefix = (unsigned)(p.prefix_tiles * p.prefix_splits * a.kv.nkv), n_own = (unsigned)(a.kv.n_seqs * p.own_tiles * p.own_splits * a.kv.nkv);
   auto launch = [&](bool many, unsigned n, int prefix) {
     if (many) hipLaunchKernelGGL((k_attn_many<DH, F32>), dim3(n), dim3(256), 0, s, a, prefix);
-    else if (p.few_rows == 16 && p.fused) hipLaunchKernelGGL((k_attn_few<DH, 16, 4, F32>), dim3(n), dim3(256), 0, s, a, prefix);
-    else if (p.few_rows == 16) hipLaunchKernelGGL((k_attn_few<DH, 16, 2, F32>), dim3(n), dim3(128), 0, s, a, prefix);
-    else if (p.fused) hipLaunchKernelGGL((k_attn_few<DH, 32, 4, F32>), dim3(n), dim3(256), 0, s, a, prefix);
-    else hipLaunchKernelGGL((k_attn_few<DH, 32, 2, F32>), dim3(n), dim3(128), 0, s, a, prefix);
+    else if (p.few_rows == 16 && p.few_waves == 1) hipLaunchKernelGGL((k_attn_few<DH, 16, 1, F32>), dim3(n), dim3(64), 0, s, a, prefix);
+    else if (p.few_rows == 16 && p.few_waves == 2) hipLaunchKernelGGL((k_attn_few<DH, 16, 2, F32>), dim3(n), dim3(128), 0, s, a, prefix);
+    else if (p.few_rows == 16) hipLaunchKernelGGL((k_attn_few<DH, 16, 4, F32>), dim3(n), dim3(256), 0, s, a, prefix);
+    else if (p.few_waves == 1) hipLaunchKernelGGL((k_attn_few<DH, 32, 1, F32>), dim3(n), dim3(64), 0, s, a, prefix);
+    else if (p.few_waves == 2) hipLaunchKernelGGL((k_attn_few<DH, 32, 2, F32>), dim3(n), dim3(128), 0, s, a, prefix);
+    else hipLaunchKernelGGL((k_attn_few<DH, 32, 4, F32>), dim3(n), dim3(256), 0, s, a, prefix);
     return hipGetLastError();
   };
   hipError_t e;
