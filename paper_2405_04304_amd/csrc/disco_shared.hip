@@ -1323,7 +1323,8 @@ hipError_t launch_append(const AppendArgs& a, bool fp32, hipStream_t s) {
 
 // Which rows share a workgroup, and how the positions are cut into ranges.  Up to 32 rows a K / V head (or a sequence) has: workgroups of that
 // many rows and two wavefronts, ranges of at least 128 positions, as many as give every compute unit one workgroup (eight beams of 40 heads, 2048
-// positions: 256 wanted 20 us, 512 21, 1024 25; four wavefronts 23, one 25).  More rows: 128 a workgroup, ranges of at least 256 positions for
+// positions: 256 wanted 20 us, 512 21, 1024 25; four wavefronts 23, one 25), and two of own positions, whose lengths differ (32 sequences of 8 K / V
+// heads with up to 700 own positions: 37 us with one, 33 with two; eight with up to 4000: 29 and 24).  More rows: 128 a workgroup, ranges of at least 256 positions for
 // two workgroups a compute unit (one where registers allow no more), but one where a range would then have no more than 512 positions: what is
 // gained is less than what the additional parts cost (4608 rows over 3001 positions: 28 us with one, 32 with two; 384 over 65537: 245 and 193).
 // A prompt and own positions that four wavefronts walk in two steps take one launch, every sequence reading the prompt by itself: 100 + 20
@@ -1333,7 +1334,7 @@ hipError_t launch_append(const AppendArgs& a, bool fp32, hipStream_t s) {
 SharedAttnPlan shared_attn_plan(int n_seqs, int n_tok, int nq, int nkv, int dh, bool fp32, int prefix_len, int max_len) {
   SharedAttnPlan p{};
   const long grp = nq / nkv, own_rows = n_tok * grp, rows = n_seqs * own_rows;
-  auto ranges = [&](bool many, long tiles, int len, int* splits, int* range) {
+  auto ranges = [&](bool many, long few_wanted, long tiles, int len, int* splits, int* range) {
     const int least = many ? 256 : 128;
     auto cut = [&](long want) {
       long n = want / tiles;
@@ -1341,7 +1342,7 @@ SharedAttnPlan shared_attn_plan(int n_seqs, int n_tok, int nq, int nkv, int dh, 
       n = n > most ? most : n;
       return n < 1 ? 1 : (n > ATTN_MAX_PARTS / 2 ? ATTN_MAX_PARTS / 2 : n);
     };
-    long n = cut(256);
+    long n = cut(many ? 256 : few_wanted);
     if (many && !(fp32 && dh == 128) && len > 512 * n) n = cut(512);
     long r = (len + n - 1) / n;
     r = (r + 63) / 64 * 64;
@@ -1359,9 +1360,9 @@ SharedAttnPlan shared_attn_plan(int n_seqs, int n_tok, int nq, int nkv, int dh, 
     if (prefix_len > 0) {
       p.prefix_many = rows > 32;
       p.prefix_tiles = p.prefix_many ? (int)((rows + 127) / 128) : 1;
-      ranges(p.prefix_many, (long)p.prefix_tiles * nkv, prefix_len, &p.prefix_splits, &p.prefix_len);
+      ranges(p.prefix_many, 256, (long)p.prefix_tiles * nkv, prefix_len, &p.prefix_splits, &p.prefix_len);
     }
-    ranges(p.own_many, (long)p.own_tiles * nkv * n_seqs, max_len, &p.own_splits, &p.own_len);
+    ranges(p.own_many, 512, (long)p.own_tiles * nkv * n_seqs, max_len, &p.own_splits, &p.own_len);
   }
   const long few = (p.own_many ? 0 : (long)n_seqs * nkv * p.own_splits) + (p.prefix_many ? 0 : (long)p.prefix_tiles * nkv * p.prefix_splits);
   p.few_waves = few > 1024 ? 1 : (p.fused && few <= 512 ? 4 : 2);
