@@ -457,7 +457,7 @@ int disco_prefill_ex(const disco_model* m, disco_kv* kv, const int32_t* dev_toke
  * sequence's own positions in pages that a table per sequence names.  The calls of a decoding step, per layer:
  * disco_append (keys and values of the new tokens into the cache, queries out), disco_attn_shared (attention); then
  * once a step disco_beam_select (next tokens) and disco_beam_reorder (page tables).  Calls with no rows return 0 and do
- * nothing.  Nothing here allocates or keeps state, so a step may be captured into a graph; calls that run at the same time
+ * nothing; a call takes up to 2^33 elements of dev_qkv or dev_q.  Nothing here allocates or keeps state, so a step may be captured into a graph; calls that run at the same time
  * need workspaces of their own.                                                                                          */
 
 enum { DISCO_F32 = 0, DISCO_BF16 = 1 };   /* element types of activations */
@@ -518,7 +518,8 @@ int disco_attn_shared(const disco_shared_kv* kv, const void* dev_q, int dtype, i
  * was finished or the token is end_token; end_token -1: no token ends a sequence) are [n_groups][k].  Candidates of probability zero (logit
  * or score -inf) are never taken; places left over hold token -1, parent -1, score -inf, done 1.  A logit that is NaN or +inf (in a beam
  * that is not finished), or such a score, makes the whole group token -1, parent -1, score NaN, done 1.
- * dev_logits: rows of vocab, row stride ld_logits >= vocab elements, any element alignment.                                                  */
+ * dev_logits: rows of vocab, row stride ld_logits >= vocab elements, any element alignment.  The results may overlap neither dev_scores and dev_done
+ * nor each other.                                                                                                                            */
 #define DISCO_MAX_BEAMS 64
 #define DISCO_BEAM_MAX_K 128
 #define DISCO_BEAM_MAX_VOCAB 1048576

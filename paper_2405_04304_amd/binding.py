@@ -418,7 +418,8 @@ class SharedKV:
 
 def disco_rope_table(n_pos: int, d_head: int, base: float = 10000.0, device="cuda", stream=None) -> torch.Tensor:
     """fp32 [n_pos, d_head / 2, 2]: (cos, sin) of every position and channel pair."""
-    t = torch.empty(n_pos, d_head // 2, 2, dtype=torch.float32, device=device)
+    t = torch.empty(max(n_pos, 0), max(d_head // 2, 0), 2, dtype=torch.float32, device=device)
+    _tensor(t, "device", _device(), torch.float32)
     _check(lib().disco_rope_table(_ptr(t), n_pos, d_head, base, _stream() if stream is None else stream))
     return t
 
@@ -489,7 +490,7 @@ def disco_beam_reorder(pages, tables, parents, tables_out, n_groups: int, n_beam
     dev = _device()
     if not pages.is_cuda or pages.get_device() != dev:
         _refuse("pages are not on the current device")
-    if pages.dim() != 5 or pages.dtype is not torch.bfloat16 or pages.shape[0] == 0 or pages.shape[2] != 2 or pages.shape[4] % page_tokens:
+    if pages.dim() != 5 or pages.dtype is not torch.bfloat16 or pages.shape[0] == 0 or pages.shape[2] != 2 or page_tokens < 1 or pages.shape[4] % page_tokens:
         _refuse("pages: bfloat16 [layers, pages, 2, K / V heads, page_tokens * d_head]")
     _, n_pages, _, heads, size = pages.shape
     if pages.stride()[1:] != (2 * heads * size, heads * size, size, 1):
@@ -545,6 +546,8 @@ def disco_step(model, kv_prompt, seqs: Sequences, tokens, logits, ws, stream=Non
 
 def disco_step_reorder(seqs: Sequences, parents, n_groups: int = 1, stream=None):
     """disco_beam_reorder of the sequences, in n_groups groups."""
+    if n_groups < 1 or seqs.n % n_groups:
+        _refuse(f"{seqs.n} sequences in {n_groups} groups")
     disco_beam_reorder(seqs.pages, seqs.tables[seqs.cur], parents, seqs.tables[1 - seqs.cur], n_groups, seqs.n // n_groups, seqs.len,
                        seqs.page_tokens, stream)
     seqs.cur = 1 - seqs.cur

@@ -77,9 +77,12 @@ SharedAttnPlan attn_plan(const disco_shared_kv* kv, bool fp32, int n_tok, int n_
   return shared_attn_plan(kv->n_seqs, n_tok, n_heads, kv->n_kv_heads, kv->d_head, fp32, kv->prefix_len, max_len == 0 || max_len > cap ? cap : max_len);
 }
 
-bool launchable(const disco_shared_kv* kv, const SharedAttnPlan& p) {
+// A launch has fewer than 2^32 threads: elements of the rows (four a thread where parts are put together, two or more where rows are appended), and
+// workgroups of up to 256.
+constexpr double MOST_ELEMENTS = 8589934592.0, MOST_WORKGROUPS = 16777216.0;
+bool launchable(const disco_shared_kv* kv, int n_tok, int n_heads, const SharedAttnPlan& p) {
   const double n = (double)kv->n_kv_heads * ((double)p.prefix_tiles * p.prefix_splits + (double)kv->n_seqs * p.own_tiles * p.own_splits);
-  return n < 2147483647.0;
+  return n < MOST_WORKGROUPS && (double)kv->n_seqs * n_tok * n_heads * kv->d_head <= MOST_ELEMENTS;
 }
 
 }  // namespace
@@ -106,6 +109,7 @@ int disco_append(const disco_shared_kv* kv, const void* dev_qkv, int dtype, int6
   if (!dev_seq && (!kv->dev_lens || n_rows % kv->n_seqs)) return fail(DISCO_EINVAL, "rows without sequences of their own need dev_lens and as many for every sequence");
   if ((rc = check_cache(kv, false))) return rc;
   const int64_t width = (int64_t)(n_heads + 2 * kv->n_kv_heads) * kv->d_head, q_width = (int64_t)n_heads * kv->d_head;
+  if ((double)n_rows * width > MOST_ELEMENTS) return fail(DISCO_EINVAL, "%d rows of %lld elements: more than 2^33 in one call", n_rows, (long long)width);
   if ((rc = check_rows(dtype, dev_qkv, ld_qkv, width, "dev_qkv")) || (rc = check_rows(dtype, dev_q, ld_q, q_width, "dev_q"))) return rc;
   const size_t es = dtype == DISCO_F32 ? 4 : 2;
   if (overlap(dev_qkv, es * ((size_t)ld_qkv * (n_rows - 1) + width), dev_q, es * ((size_t)ld_q * (n_rows - 1) + q_width)))
@@ -150,7 +154,7 @@ int disco_attn_shared(const disco_shared_kv* kv, const void* dev_q, int dtype, i
     return fail(DISCO_EINVAL, "dev_out overlaps dev_q");
   SharedAttnArgs a{};
   a.plan = attn_plan(kv, dtype == DISCO_F32, n_tok, n_heads, max_len);
-  if (!launchable(kv, a.plan)) return fail(DISCO_EINVAL, "more workgroups than a launch takes");
+  if (!launchable(kv, n_tok, n_heads, a.plan)) return fail(DISCO_EINVAL, "more workgroups than a launch takes");
   if (a.plan.bytes > 0) {
     if (!dev_ws || !aligned(dev_ws, 256)) return fail(DISCO_EINVAL, "workspace null or not 256-byte aligned");
     if (ws_bytes < a.plan.bytes) return fail(DISCO_EINVAL, "workspace of %zu bytes, %zu needed", ws_bytes, a.plan.bytes);
@@ -192,6 +196,15 @@ int disco_beam_select(const void* dev_logits, int dtype, int64_t ld_logits, int 
   if (!aligned(dev_logits, dtype == DISCO_F32 ? 4 : 2) || !aligned(dev_scores, 4) || !aligned(dev_done, 4) || !aligned(dev_tokens, 4) || !aligned(dev_parents, 4) ||
       !aligned(dev_scores_out, 4) || !aligned(dev_done_out, 4) || !aligned(dev_ws, 256))
     return fail(DISCO_EINVAL, "misaligned pointer");
+  // (a group's results are written while another's scores are read)
+  const size_t in = 4 * (size_t)n_groups * n_beams, out = 4 * (size_t)n_groups * k;
+  const void* outs[4] = {dev_tokens, dev_parents, dev_scores_out, dev_done_out};
+  for (int i = 0; i < 4; ++i) {
+    if (!outs[i]) continue;
+    bool shared = overlap(outs[i], out, dev_scores, in) || (dev_done && overlap(outs[i], out, dev_done, in));
+    for (int j = 0; j < i; ++j) shared |= overlap(outs[i], out, outs[j], out);
+    if (shared) return fail(DISCO_EINVAL, "a result overlaps dev_scores, dev_done or another result");
+  }
   const size_t need = disco_beam_select_bytes(n_groups, n_beams, vocab, k), rows = (size_t)n_groups * n_beams, per_row = (size_t)beam_units((int)rows, vocab);
   if (ws_bytes < need) return fail(DISCO_EINVAL, "workspace of %zu bytes, %zu needed", ws_bytes, need);
   BeamSelectArgs a{};
@@ -211,6 +224,7 @@ int disco_beam_reorder(void* dev_pages, int n_layers, int64_t layer_stride, int 
   if (n_layers < 1 || n_layers > 65535 || n_pages < 1 || page_elems < 8 || page_elems % 8 || layer_stride < 0 || layer_stride % 8 ||
       (n_layers > 1 && layer_stride / page_elems < n_pages))
     return fail(DISCO_EINVAL, "bad page pool");
+  if ((double)n_layers * n_beams * ((double)page_elems / 32768 + 1) >= MOST_WORKGROUPS) return fail(DISCO_EINVAL, "more copies than a launch takes");
   if (n_groups == 0) return DISCO_OK;
   if (!dev_pages || !dev_tables || !dev_tables_out || !dev_parents) return fail(DISCO_EINVAL, "null argument");
   if (!aligned(dev_pages, 16) || !aligned(dev_tables, 4) || !aligned(dev_tables_out, 4) || !aligned(dev_parents, 4)) return fail(DISCO_EINVAL, "misaligned pointer");
@@ -285,10 +299,9 @@ int disco_step(const disco_model* m, disco_kv* kv_prompt, const disco_shared_kv*
   if (layer_stride < 0 || layer_stride % 8 || (d.n_layers > 1 && layer_stride / page_elems < k.n_pages)) return fail(DISCO_EINVAL, "bad page pool");
   const StepWs ws = carve_step(m, k, dev_ws);
   if (ws_bytes < ws.total) return fail(DISCO_EINVAL, "workspace of %zu bytes, %zu needed", ws_bytes, ws.total);
-  if (kv_prompt->dev_rope && !kv_prompt->rope_ready) {
+  // An empty prompt's table may be unwritten.  Every step writes it then (the same values): another stream's step does not wait for this one's.
+  if (kv_prompt->dev_rope && !kv_prompt->rope_ready)
     HIP_TRY(launch_rope_fill(kv_prompt->dev_rope, kv_prompt->capacity, d.d_head, d.rope_base, s), "rotary table launch");
-    kv_prompt->rope_ready = true;
-  }
   const Ws& b = ws.base;
   const int split_o = gemm_split_for(d.d_model, m->d_q / 32, n), split_dn = gemm_split_for(d.d_model, d.d_ff / 32, n);
 
@@ -317,7 +330,7 @@ int disco_step(const disco_model* m, disco_kv* kv_prompt, const disco_shared_kv*
   ap.qkv = ws.qkv; ap.ld = m->d_qkv; ap.rows = n; ap.nq = d.n_heads; ap.n_tok = 1; ap.rope = kv_prompt->dev_rope; ap.q = ws.q; ap.ld_q = m->d_q;
   SharedAttnArgs at{};
   at.plan = attn_plan(&k, true, 1, d.n_heads, 0);
-  if (!launchable(&k, at.plan)) return fail(DISCO_EINVAL, "more workgroups than a launch takes");
+  if (!launchable(&k, 1, d.n_heads, at.plan)) return fail(DISCO_EINVAL, "more workgroups than a launch takes");
   at.q = ws.q; at.ld_q = m->d_q; at.n_tok = 1; at.nq = d.n_heads; at.scale = 1.0f / sqrtf((float)d.d_head); at.panels = b.xattn;
   at.part = static_cast<float*>(ws.attn); at.ml = reinterpret_cast<float2*>(at.part + (size_t)at.plan.parts * n * m->d_q);
   for (int l = 0; l < d.n_layers; ++l) {

@@ -140,3 +140,34 @@ def test_binding_refuses_tensors_it_cannot_hand_over():
         B.disco_beam_select(torch.zeros(4, 10), torch.zeros(4), 1, 4, 4, tables, tables, torch.zeros(4), torch.zeros(256, dtype=torch.uint8))
     with pytest.raises(B.DiscoError, match="device"):
         B.disco_beam_reorder(pages[None], tables, tables, tables, 1, 2, 3, 16)
+
+
+def test_select_refuses_results_that_overlap():
+    """A group's results are written while another group's scores are read (and its own flags, by other lanes)."""
+    base = dict(n_groups=2, n_beams=4, k=8, end=1, scores=FAKE + 8 * GB, done=FAKE + 9 * GB, tokens=FAKE + 10 * GB, parents=FAKE + 11 * GB, scores_out=FAKE + 12 * GB,
+                done_out=FAKE + 13 * GB)
+    for over in (dict(scores_out=base["scores"]), dict(scores_out=base["scores"] + 28), dict(scores_out=base["scores"] - 60), dict(done_out=base["done"]),
+                 dict(tokens=base["done"] + 4), dict(tokens=base["parents"]), dict(parents=base["scores_out"] + 60), dict(done_out=base["tokens"] - 4)):
+        assert _select(**{**base, **over}) == B.EINVAL and "overlap" in B.last_error(), over
+
+
+def test_calls_larger_than_a_launch():
+    """More threads than 2^32 are refused, not cut off."""
+    for heads, d in ((512, 128), (1024, 64)):           # 2^24 rows of 2^16 and more elements
+        kv = _kv(d_head=d, n_kv_heads=heads, n_seqs=1, dev_prefix=None, prefix_len=0)
+        assert _append(kv, n_heads=heads, n_rows=1 << 24, ld_qkv=3 * heads * d, ld_q=heads * d, qkv=FAKE, q=FAKE + (1 << 46), n_rope=1 << 20) == B.EINVAL
+        assert "2^33" in B.last_error()
+    wide = _kv(d_head=128, n_kv_heads=1024, n_seqs=65535, dev_prefix=None, prefix_len=0)
+    assert _attn(wide, n_heads=1024, ld_q=1 << 17, ld_out=1 << 17, out=FAKE + (1 << 46), ws_bytes=1 << 60) == B.EINVAL and "launch" in B.last_error()
+    assert _reorder(page_elems=1 << 40, layer_stride=1 << 46) == B.EINVAL
+    assert _reorder(n_layers=65535, n_beams=64, page_elems=1 << 20, layer_stride=1 << 26) == B.EINVAL and "launch" in B.last_error()
+
+
+def test_attention_plan_holds_over_its_arguments():
+    """Workspaces of calls from one token of one sequence to many: never none, whole multiples of 256 bytes."""
+    for seqs in (1, 3, 40, 900):
+        for prefix in (0, 1, 129, 4097, 70000):
+            for tok in (1, 7, 16):
+                got = [B.lib().disco_attn_shared_bytes(C.byref(_kv(n_seqs=seqs, prefix_len=prefix, n_prefix_pages=5000, n_kv_heads=kvh, table_ld=300)), tok, 4 * kvh, n)
+                       for kvh in (1, 8) for n in (0, 1, 300)]
+                assert all(x >= 256 and x % 256 == 0 for x in got)
