@@ -353,8 +353,11 @@ def _bad_tensor(t, what, dtype, numel):
 
 
 def _device() -> int:
-    """The current device, -1 where there is none."""
-    return torch.cuda.current_device() if torch.cuda.is_initialized() or torch.cuda.is_available() else -1
+    """The current device, -1 where there is none (what torch.cuda.current_device asks, without its checks)."""
+    try:
+        return torch._C._cuda_getDevice()
+    except RuntimeError:
+        return -1
 
 
 def _tensor(t, what: str, dev: int, dtype, numel: int = 0) -> int:
@@ -371,12 +374,13 @@ def _rows(t, what: str, dev: int, n: int, width: int):
     code = _DTYPES.get(t.dtype)
     if code is None:
         _refuse(f"{what} has type {t.dtype}: float32 or bfloat16")
-    if t.dim() != 2 or t.shape[0] < n or t.shape[1] < width:
-        _refuse(f"{what} has shape {tuple(t.shape)}, ({n}, {width}) needed")
+    shape = t.shape
+    if len(shape) != 2 or shape[0] < n or shape[1] < width:
+        _refuse(f"{what} has shape {tuple(shape)}, ({n}, {width}) needed")
     ld, one = t.stride()
-    if one != 1 and t.shape[1] != 1:
+    if one != 1 and shape[1] != 1:
         _refuse(f"{what}: the elements of a row are not contiguous")
-    return t.data_ptr(), code, ld if n > 1 else max(ld, t.shape[1])
+    return t.data_ptr(), code, ld if n > 1 else max(ld, shape[1])
 
 
 def _raw_stream(dev: int, stream) -> int:
@@ -490,17 +494,21 @@ def disco_beam_reorder(pages, tables, parents, tables_out, n_groups: int, n_beam
     dev = _device()
     if not pages.is_cuda or pages.get_device() != dev:
         _refuse("pages are not on the current device")
-    if pages.dim() != 5 or pages.dtype is not torch.bfloat16 or pages.shape[0] == 0 or pages.shape[2] != 2 or page_tokens < 1 or pages.shape[4] % page_tokens:
+    shape = pages.shape
+    if len(shape) != 5 or pages.dtype is not torch.bfloat16 or shape[0] == 0 or shape[2] != 2 or page_tokens < 1 or shape[4] % page_tokens:
         _refuse("pages: bfloat16 [layers, pages, 2, K / V heads, page_tokens * d_head]")
-    _, n_pages, _, heads, size = pages.shape
-    if pages.stride()[1:] != (2 * heads * size, heads * size, size, 1):
+    layers, n_pages, _, heads, size = shape
+    layer, *page = pages.stride()
+    if page != [2 * heads * size, heads * size, size, 1]:
         _refuse("pages: the pages of a layer are not contiguous")
-    if tables.dim() != 2 or tables.shape[0] < n_groups * n_beams:
+    shape = tables.shape
+    if len(shape) != 2 or shape[0] < n_groups * n_beams:
         _refuse("tables: [sequences, pages]")
-    _check(lib().disco_beam_reorder(pages.data_ptr(), pages.shape[0], pages.stride(0), n_pages, 2 * heads * size,
-                                    _tensor(tables, "tables", dev, torch.int32), _tensor(tables_out, "tables_out", dev, torch.int32, tables.numel()),
-                                    tables.shape[1], _tensor(parents, "parents", dev, torch.int32, n_groups * n_beams), n_groups, n_beams, length,
-                                    page_tokens, _raw_stream(dev, stream)))
+    rows, cols = shape
+    _check(lib().disco_beam_reorder(pages.data_ptr(), layers, layer, n_pages, 2 * heads * size, _tensor(tables, "tables", dev, torch.int32),
+                                    _tensor(tables_out, "tables_out", dev, torch.int32, rows * cols), cols,
+                                    _tensor(parents, "parents", dev, torch.int32, n_groups * n_beams), n_groups, n_beams, length, page_tokens,
+                                    _raw_stream(dev, stream)))
 
 
 class Sequences:
