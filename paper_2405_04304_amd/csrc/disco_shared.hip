@@ -900,7 +900,8 @@ __global__ __launch_bounds__(256) void k_shared_merge(SharedAttnArgs a) {
 __device__ __forceinline__ float logit(const float* p) { return *p; }
 __device__ __forceinline__ float logit(const bf16_t* p) { return bf16_to_f32(*p); }
 
-// A bound that at least k of the wavefront's 256 values reach (0 where fewer are not 0): the k-th largest but for its last 12 bits.
+// A bound that at least k of the wavefront's 256 values reach (0 where fewer are not 0): the k-th largest but for its last 12 bits (stopping
+// once few enough reach the bound makes the list longer: half a microsecond slower).
 __device__ __forceinline__ uint32_t kth_bound(const uint32_t (&m)[4], const int k) {
   const uint32_t top = wave_max_u32(max(max(m[0], m[1]), max(m[2], m[3])));
   uint32_t cur = 0;
@@ -937,12 +938,19 @@ __device__ __forceinline__ void wave_top_k(Visit visit, Narrow narrow, Key key, 
     visit(append);
   }
   wave_lds_fence();
-  for (int i = lane; i < n; i += 64) list[i] = key(list[i]);
+  const int n_pad = (n + 7) & ~7;
+  for (int i = lane; i < n_pad; i += 64) list[i] = i < n ? key(list[i]) : 0ull;
   wave_lds_fence();
   for (int i = lane; i < n; i += 64) {
     const unsigned long long mine = list[i];
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += list[j] > mine ? 1 : 0;
+    for (int j = 0; j < n_pad; j += 8) {                        // (eight reads on their way at once)
+      unsigned long long x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = list[j + u];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) rank += x[u] > mine ? 1 : 0;
+    }
     if (rank < k) out[rank] = mine;
   }
   for (int i = n + lane; i < k; i += 64) out[i] = 0;
@@ -1099,7 +1107,14 @@ __global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
   if (t == 0) s_bad = 0;
   __syncthreads();
   for (int b = w; b < a.n_beams; b += nw) {
-    const int row = g * a.n_beams + b;
+    const int row = g * a.n_beams + b, total = a.units * k;
+    // what the row needs is requested together: candidates (in registers where that holds all), statistics, score
+    const unsigned long long* src = a.cand + (size_t)row * a.units * k;
+    unsigned long long r[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) r[e] = total <= 64 * 16 && e * 64 + lane < total ? src[e * 64 + lane] : 0ull;
+    const float2* st = a.stats + (size_t)row * a.units;
+    const float2 mine = lane < a.units ? st[lane] : make_float2(-INFINITY, 0.f);
     const float score = a.scores[row];
     bool bad = !(score < INFINITY);
     int n = 0;
@@ -1107,13 +1122,12 @@ __global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
       n = score > -INFINITY ? 1 : 0;
       if (lane == 0) cand[b * k] = BeamCand{(double)score, a.end_token, 0};
     } else {
-      const float2* st = a.stats + (size_t)row * a.units;
-      float m = -INFINITY;
-      for (int c = lane; c < a.units; c += 64) m = fmaxf(m, st[c].x);
+      float m = mine.x;
+      for (int c = lane + 64; c < a.units; c += 64) m = fmaxf(m, st[c].x);
       m = key_f32(wave_max_u32(f32_key(m)));
       double sum = 0.0;
       for (int c = lane; c < a.units; c += 64) {
-        const float2 s = st[c];
+        const float2 s = c == lane ? mine : st[c];
         bad |= !(s.y < INFINITY);
         if (s.x > -INFINITY) sum += (double)s.y * exp((double)s.x - (double)m);
       }
@@ -1122,16 +1136,10 @@ __global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
       bad = __any(bad);
       const double off = (double)score - ((double)m + log(sum));
       if (!bad && score > -INFINITY && m > -INFINITY) {
-        const unsigned long long* src = a.cand + (size_t)row * a.units * k;
-        const int total = a.units * k;
         uint32_t q[4] = {0u, 0u, 0u, 0u};
-        if (total <= 64 * 16) {                                 // in registers, all on their way at once
-          unsigned long long r[16];
+        if (total <= 64 * 16) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            r[e] = e * 64 + lane < total ? src[e * 64 + lane] : 0ull;
-            q[e & 3] = max(q[e & 3], (uint32_t)(r[e] >> 32));
-          }
+          for (int e = 0; e < 16; ++e) q[e & 3] = max(q[e & 3], (uint32_t)(r[e] >> 32));
           wave_top_k_keys<16>(16, [&](int e) { return r[e]; }, kth_bound(q, k), k, list, keys);
         } else {
           auto at = [&](int e) { return e * 64 + lane < total ? src[e * 64 + lane] : 0ull; };
@@ -1158,11 +1166,13 @@ __global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
   for (int b = 0; b < a.n_beams; ++b) have += s_n[b];
   // rank of every candidate: its place in its own row's list and, counted row by row, the better ones of the others (lists in order)
   const int n_all = a.n_beams * k;
-  for (int i = t; i < n_all; i += blockDim.x) cand[i].rank = i % k;
+  const float per_beam = 1.0f / (float)k, per_set = 1.0f / (float)n_all;
+  auto part = [](const int i, const float by) { return (int)(((float)i + 0.5f) * by); };    // i / n for i up to 2^19 and quotients up to 64: off by less than 0.5 / n
+  for (int i = t; i < n_all; i += blockDim.x) cand[i].rank = i - part(i, per_beam) * k;
   __syncthreads();
   if (!bad)
     for (int i = t; i < n_all * a.n_beams; i += blockDim.x) {
-      const int c = i % n_all, o = i / n_all, b = c / k;
+      const int o = part(i, per_set), c = i - o * n_all, b = part(c, per_beam);
       if (o == b || c - b * k >= s_n[b]) continue;
       const double mine = cand[c].s;
       int lo = 0, hi = s_n[o];
@@ -1175,7 +1185,7 @@ __global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
     }
   __syncthreads();
   for (int i = t; i < n_all; i += blockDim.x) {
-    const int b = i / k;
+    const int b = part(i, per_beam);
     const BeamCand c = cand[i];
     if (bad || i - b * k >= s_n[b] || c.rank >= k) continue;
     const size_t at = (size_t)g * k + c.rank;
