@@ -896,6 +896,9 @@ __global__ __launch_bounds__(256) void k_shared_merge(SharedAttnArgs a) {
 // their sum of exponentials and the k largest in order; a workgroup per group merges the units of each row (a wavefront a row) and
 // ranks the rows' k best against each other.  The k largest of many come from a bound (the k-th largest of 256 partial maxima), a
 // list of what reaches it, and the rank of each entry of the list: no sort and no rounds of k.
+// Units: bound by the instructions of a logit (unpacking, maximum, difference, exponential at a quarter of the rate, sum): 64 groups of sixteen beams over 128001
+// bf16 logits, 262 MB, 63 us, 4.2 TB/s.  Merge: one workgroup a group, a chain of round trips (candidates from other XCDs 2 us, the row's list 2 us, logarithm
+// and keys 1 us, ranks between the rows 1.5 us): 6 us for one group of four beams, 9 for eight of eight, 11 for the 64 of sixteen.
 
 __device__ __forceinline__ float logit(const float* p) { return *p; }
 __device__ __forceinline__ float logit(const bf16_t* p) { return bf16_to_f32(*p); }
@@ -915,6 +918,7 @@ __device__ __forceinline__ uint32_t kth_bound(const uint32_t (&m)[4], const int 
 }
 
 constexpr int BEAM_LIST = 256;       // keys of a wavefront's list
+constexpr int BEAM_STAGE = 64;       // quarters of lanes' logits that are kept in LDS
 
 // The k largest keys of a wavefront, in order, to out[0 .. k) (0 behind the last).  visit(f): f(whether the lane's e-th entry reaches the bound,
 // entry) for every e; narrow(): makes the bound the k-th largest key itself; key(entry): distinct.  At least k entries reach the bound, or all do.
@@ -955,29 +959,73 @@ __device__ __forceinline__ void wave_top_k(Visit visit, Narrow narrow, Key key, 
   }
   for (int i = n + lane; i < k; i += 64) out[i] = 0;
 }
-// The same over keys at(e), n_e a lane.
-template <int UNROLL, typename At>
-__device__ __forceinline__ void wave_top_k_keys(const int n_e, At at, const uint32_t bound, const int k, unsigned long long* list, unsigned long long* out) {
+// The same over 64 x 16 keys r in registers.
+__device__ __forceinline__ void wave_top_k_keys(const unsigned long long (&r)[16], const uint32_t bound, const int k, unsigned long long* list, unsigned long long* out) {
   unsigned long long least = (unsigned long long)max(bound, 1u) << 32;
   wave_top_k([&](auto f) {
-#pragma unroll UNROLL
-    for (int e = 0; e < n_e; ++e) { const unsigned long long x = at(e); f(x >= least, [&]() { return x; }); }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) f(r[e] >= least, [&]() { return r[e]; });
   }, [&]() {
     least = 0;
     for (int bit = 63; bit >= 0; --bit) {
       const unsigned long long t = least | (1ull << bit);
       int c = 0;
-#pragma unroll UNROLL
-      for (int e = 0; e < n_e; ++e) c += __popcll(__ballot(at(e) >= t));
+#pragma unroll
+      for (int e = 0; e < 16; ++e) c += __popcll(__ballot(r[e] >= t));
       if (c >= k) least = t;
     }
     if (least == 0) least = 1;
   }, [](unsigned long long x) { return x; }, k, list, out);
 }
+// The same over `total` keys in memory, of which at least k reach the bound, or all that are not 0.  While more than the list holds reach it, the k-th
+// largest of those in the list becomes the bound: at least k reach that, and BEAM_LIST - k fewer than before.
+__device__ __forceinline__ void wave_top_k_memory(const unsigned long long* src, const int total, const uint32_t bound, const int k, unsigned long long* list, unsigned long long* out) {
+  const int lane = threadIdx.x & 63;
+  unsigned long long least = (unsigned long long)max(bound, 1u) << 32;
+  int n;
+  auto rank_of = [&](const unsigned long long mine, const int end) {
+    int rank = 0;
+    for (int j = 0; j < end; j += 8)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) rank += list[j + u] > mine ? 1 : 0;
+    return rank;
+  };
+  for (;;) {
+    n = 0;
+    for (int i = lane; i - lane < total; i += 64 * 8) {
+      unsigned long long x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = i + 64 * u < total ? src[i + 64 * u] : 0ull;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const unsigned long long hit = __ballot(x[u] >= least);
+        const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hit, 0));
+        if (x[u] >= least && at < BEAM_LIST) list[at] = x[u];
+        n += __popcll(hit);
+      }
+    }
+    wave_lds_fence();
+    if (n <= BEAM_LIST) break;
+    unsigned long long kth = 0;
+    for (int i = lane; i < BEAM_LIST; i += 64)
+      if (rank_of(list[i], BEAM_LIST) == k - 1) kth = list[i];
+    least = __shfl(kth, __ffsll((unsigned long long)__ballot(kth != 0)) - 1);
+    wave_lds_fence();
+  }
+  const int n_pad = (n + 7) & ~7;
+  for (int i = n + lane; i < n_pad; i += 64) list[i] = 0;
+  wave_lds_fence();
+  for (int i = lane; i < n; i += 64) {
+    const unsigned long long mine = list[i];
+    const int rank = rank_of(mine, n_pad);
+    if (rank < k) out[rank] = mine;
+  }
+  for (int i = n + lane; i < k; i += 64) out[i] = 0;
+}
 
 // E logits of a lane in registers, eight consecutive ones at a time, in 16-byte loads wherever the row starts (rows of an odd vocabulary do not
 // start at 16 bytes); -inf beyond the row.  bf16 logits stay packed and are unpacked in every pass over them: half the registers, so that
-// seven wavefronts share a SIMD instead of three.
+// six wavefronts share a SIMD instead of three (1024 rows of 128001: 63 us; four 72, five 64, seven, with registers spilled, 71).
 template <typename T, int E> struct UnitLogits;
 template <int E> struct UnitLogits<float, E> {
   float v[E];
@@ -994,6 +1042,10 @@ template <int E> struct UnitLogits<float, E> {
   }
   __device__ __forceinline__ float operator[](int e) const { return v[e]; }
   __device__ __forceinline__ void next_pass() {}
+  __device__ __forceinline__ void store_quarter(float* to, const int q) const {
+#pragma unroll
+    for (int e = 0; e < E / 4; e += 4) *reinterpret_cast<f32x4*>(to + e) = f32x4{v[q * E / 4 + e], v[q * E / 4 + e + 1], v[q * E / 4 + e + 2], v[q * E / 4 + e + 3]};
+  }
 };
 template <int E> struct UnitLogits<bf16_t, E> {
   uint32_t v[E / 2];
@@ -1010,6 +1062,10 @@ template <int E> struct UnitLogits<bf16_t, E> {
     }
   }
   __device__ __forceinline__ float operator[](int e) const { return __uint_as_float((e & 1) ? v[e >> 1] & 0xffff0000u : v[e >> 1] << 16); }
+  __device__ __forceinline__ void store_quarter(bf16_t* to, const int q) const {
+#pragma unroll
+    for (int e = 0; e < E / 4; e += 4) *reinterpret_cast<uint2*>(to + e) = make_uint2(v[(q * E / 4 + e) / 2], v[(q * E / 4 + e) / 2 + 1]);
+  }
   __device__ __forceinline__ void next_pass() {                 // what was unpacked is forgotten
 #pragma unroll
     for (int e = 0; e < E / 2; ++e) asm volatile("" : "+v"(v[e]));
@@ -1017,8 +1073,11 @@ template <int E> struct UnitLogits<bf16_t, E> {
 };
 
 template <typename T, int E>
-__global__ __launch_bounds__(256, E == 64 ? (sizeof(T) == 2 ? 5 : 3) : 8) void k_beam_units(BeamSelectArgs a) {
+__global__ __launch_bounds__(256, E == 64 ? (sizeof(T) == 2 ? 6 : 3) : 8) void k_beam_units(BeamSelectArgs a) {
+  constexpr int Q = E / 4;
   __shared__ unsigned long long lists[4][BEAM_LIST];
+  __shared__ __align__(16) T staged[4][BEAM_STAGE * Q];
+  __shared__ unsigned char staged_from[4][BEAM_STAGE];          // quarter * 64 + lane
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int id = blockIdx.x * 4 + w;
   if (id >= a.n_groups * a.n_beams * a.units) return;
@@ -1052,7 +1111,38 @@ __global__ __launch_bounds__(256, E == 64 ? (sizeof(T) == 2 ? 5 : 3) : 8) void k
   float least = bound == 0 ? -3.402823466e38f : key_f32(bound), edge = NAN;
   int upto = 0;
   const int at0 = first + lane * 8;                             // index of e: at0 + 64 (e & ~7) + (e & 7)
+  // Only quarters whose maximum reaches the bound hold entries, about k of the 256: those go to LDS, and a pass over what is there takes the place
+  // of one over every register (1024 rows of 128001: 63 us against 68).
+  int n_staged = 0;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) n_staged += __popcll(__ballot(m[q] >= max(bound, 1u)));
+  const bool stage = n_staged <= BEAM_STAGE;
+  if (stage) {
+    int n = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const bool mine = m[q] >= max(bound, 1u);
+      const unsigned long long hit = __ballot(mine);
+      if (mine) {
+        const int slot = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hit, 0));
+        v.store_quarter(&staged[w][slot * Q], q);
+        staged_from[w][slot] = (unsigned char)(q * 64 + lane);
+      }
+      n += __popcll(hit);
+    }
+    wave_lds_fence();
+  }
   wave_top_k([&](auto f) {
+    if (stage) {
+      for (int i0 = 0; i0 < n_staged * Q; i0 += 64) {
+        const int i = i0 + lane;
+        const bool in = i < n_staged * Q;
+        const int from = in ? staged_from[w][i / Q] : 0, e = (from >> 6) * Q + i % Q, at = first + (from & 63) * 8 + (e & ~7) * 64 + (e & 7);
+        const float y = in ? logit(&staged[w][i]) : -INFINITY;
+        f(y >= least && !(y == edge && at > upto), [&]() { return ((unsigned long long)__float_as_uint(y) << 32) | (uint32_t)at; });
+      }
+      return;
+    }
     v.next_pass();
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -1095,24 +1185,37 @@ __global__ __launch_bounds__(256, E == 64 ? (sizeof(T) == 2 ? 5 : 3) : 8) void k
 
 struct BeamCand { double s; int token; int rank; };   // of one row; equal keys by the lower token
 
-// LDS: candidates [beam][k], keys [wavefront][k], lists [wavefront][BEAM_LIST].  Workgroup of a wavefront per row, up to sixteen.
+// LDS: candidates [beam][k], keys [wavefront][k], lists [wavefront][BEAM_LIST].  Workgroup of a wavefront per row, up to sixteen.  LONG: the units'
+// candidates of a row are more than the registers hold (1024).
+template <bool LONG>
 __global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
   extern __shared__ __align__(16) char smem[];
   __shared__ int s_bad;
   __shared__ int s_n[DISCO_BEAM_MAX_ROWS];
   const int g = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6, nw = blockDim.x >> 6, k = a.k;
+  const float per_unit = 1.0f / (float)a.units;
   BeamCand* cand = reinterpret_cast<BeamCand*>(smem);
   unsigned long long* keys = reinterpret_cast<unsigned long long*>(cand + a.n_beams * k) + w * k;
   unsigned long long* list = reinterpret_cast<unsigned long long*>(cand + a.n_beams * k) + nw * k + w * BEAM_LIST;
+  auto part = [](const int i, const float by) { return (int)(((float)i + 0.5f) * by); };    // i / n for i up to 2^19 and quotients up to 1024: off by less than 0.5 / n
   if (t == 0) s_bad = 0;
   __syncthreads();
   for (int b = w; b < a.n_beams; b += nw) {
     const int row = g * a.n_beams + b, total = a.units * k;
-    // what the row needs is requested together: candidates (in registers where that holds all), statistics, score
+    // What the row needs is requested together: candidates (LONG: the best of every unit, next to each other so that the 256 maxima below are those
+    // of the best few), statistics, score.
     const unsigned long long* src = a.cand + (size_t)row * a.units * k;
     unsigned long long r[16];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) r[e] = total <= 64 * 16 && e * 64 + lane < total ? src[e * 64 + lane] : 0ull;
+    for (int e = 0; e < 16; ++e) {
+      const int i = e * 64 + lane;
+      if constexpr (LONG) {
+        const int pos = part(i, per_unit);
+        r[e] = pos < 64 * 16 / a.units ? src[(i - pos * a.units) * k + pos] : 0ull;
+      } else {
+        r[e] = i < total ? src[i] : 0ull;
+      }
+    }
     const float2* st = a.stats + (size_t)row * a.units;
     const float2 mine = lane < a.units ? st[lane] : make_float2(-INFINITY, 0.f);
     const float score = a.scores[row];
@@ -1137,18 +1240,11 @@ __global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
       const double off = (double)score - ((double)m + log(sum));
       if (!bad && score > -INFINITY && m > -INFINITY) {
         uint32_t q[4] = {0u, 0u, 0u, 0u};
-        if (total <= 64 * 16) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) q[e & 3] = max(q[e & 3], (uint32_t)(r[e] >> 32));
-          wave_top_k_keys<16>(16, [&](int e) { return r[e]; }, kth_bound(q, k), k, list, keys);
-        } else {
-          auto at = [&](int e) { return e * 64 + lane < total ? src[e * 64 + lane] : 0ull; };
-          const int n_e = (total + 63) / 64;
-          for (int e = 0; e < n_e; e += 4)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) q[u] = max(q[u], (uint32_t)(at(e + u) >> 32));
-          wave_top_k_keys<1>(n_e, at, kth_bound(q, k), k, list, keys);
-        }
+        for (int e = 0; e < 16; ++e) q[e & 3] = max(q[e & 3], (uint32_t)(r[e] >> 32));
+        const uint32_t bound = kth_bound(q, k);
+        if constexpr (LONG) wave_top_k_memory(src, total, bound, k, list, keys);
+        else wave_top_k_keys(r, bound, k, list, keys);
         wave_lds_fence();
         for (int i = lane; i < k; i += 64) {
           const unsigned long long key = keys[i];
@@ -1167,7 +1263,6 @@ __global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
   // rank of every candidate: its place in its own row's list and, counted row by row, the better ones of the others (lists in order)
   const int n_all = a.n_beams * k;
   const float per_beam = 1.0f / (float)k, per_set = 1.0f / (float)n_all;
-  auto part = [](const int i, const float by) { return (int)(((float)i + 0.5f) * by); };    // i / n for i up to 2^19 and quotients up to 64: off by less than 0.5 / n
   for (int i = t; i < n_all; i += blockDim.x) cand[i].rank = i - part(i, per_beam) * k;
   __syncthreads();
   if (!bad)
@@ -1431,7 +1526,8 @@ hipError_t launch_beam_select(const BeamSelectArgs& a, bool fp32, hipStream_t s)
   auto lds_bytes = [&]() { return sizeof(BeamCand) * a.n_beams * a.k + sizeof(unsigned long long) * nw * (a.k + BEAM_LIST); };
   while (nw > 4 && lds_bytes() > (size_t)150 << 10) nw /= 2;    // 64 beams of 128: 128 KiB for the candidates
   const size_t lds = lds_bytes();
-  hipLaunchKernelGGL(k_beam_merge, dim3((unsigned)a.n_groups), dim3(64 * nw), lds, s, a);
+  if (a.units * a.k <= 64 * 16) hipLaunchKernelGGL(k_beam_merge<false>, dim3((unsigned)a.n_groups), dim3(64 * nw), lds, s, a);
+  else hipLaunchKernelGGL(k_beam_merge<true>, dim3((unsigned)a.n_groups), dim3(64 * nw), lds, s, a);
   return hipGetLastError();
 }
 

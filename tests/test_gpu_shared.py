@@ -380,3 +380,26 @@ def test_reorder_pages_outside_the_pool_and_strided_layers():
         w_t, w_p = R.reorder(pool, tables, parents, 1, 4, 20, 16)
         assert torch.equal(out.cpu(), w_t)
         assert torch.equal(p[:, :12].cpu().view(torch.int16), w_p.view(torch.int16)) and torch.equal(p[:, 12:].cpu(), wide[:, 12:])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("kind", ["random", "few ranges", "rising", "equal", "steps"])
+@pytest.mark.parametrize("beams,vocab,k", [(3, 70001, 128), (64, 140003, 64), (2, 3000, 128)])
+def test_select_where_the_best_lie_close_together(beams, vocab, k, kind, dtype):
+    """Many candidates: the best of a row in a few ranges of its vocabulary (a mask), all in its last one, all equal, a few values only."""
+    g = _gen(vocab + k)
+    logits = torch.randn(beams, vocab, generator=g)
+    if kind == "few ranges":
+        mask = torch.ones(vocab, dtype=torch.bool)
+        for first in (100, vocab // 2, vocab - 900):
+            mask[first:first + 700] = False
+        logits[:, mask] = -math.inf
+    elif kind == "rising":
+        logits = torch.linspace(-4.0, 4.0, vocab).repeat(beams, 1)
+    elif kind == "equal":
+        logits = torch.full((beams, vocab), -1.25)
+    elif kind == "steps":
+        logits = torch.randint(-3, 3, (beams, vocab), generator=g).float()
+    logits = logits.to(dtype)
+    scores = -torch.arange(beams, dtype=F32) / 8
+    _check_select(_select(logits, scores, 1, beams, k), R.select(logits, scores, 1, beams, k))
