@@ -33,6 +33,11 @@ __device__ __forceinline__ void store4(bf16_t* p, float4 v) { *reinterpret_cast<
 // ---------------------------------------------------------------------------------------------
 // append
 // ---------------------------------------------------------------------------------------------
+//
+// y = rotate(norm(x)) for query and key heads, K to [token][channel] blocks, V to [channel][token] blocks, one pass.  Norm and rotation in fp32, one rounding
+// to bf16 at the cache's entry (queries: to their own type).  Bytes only: 5999 rows of 3 x 40 heads of 128 in bf16, 372 MB, take 86 us, 4.3 TB/s; what is left to the
+// copy's rate (73 us) is the tiles of V, whose loads end at a barrier before their stores begin.  Small calls are three dependent round trips (position,
+// page, entry): 2.9 us for four rows, 6.4 us for 192.
 
 // Where row i goes: its sequence's own position and the page that holds it; pos < 0: nowhere (padding, or outside the tables).
 struct RowPlace { int seq, pos, page; };
@@ -225,14 +230,13 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs a, int n_heads_wgs, i
 // attention
 // ---------------------------------------------------------------------------------------------
 //
-// Row r = (sequence * n_tok + token) * group + query head of a K / V head's rows.  A workgroup takes 32 * WR rows of one K / V head and a
-// range of positions, of the prompt (then the rows are those of all sequences) or of one sequence's own; WT wavefronts share the
-// positions of a tile.  Per 32 positions and 32 rows:
-//   S^T[position][row] = K . Q^T,   O^T[channel][row] += V^T . P^T       (32x32x16 bf16, fp32 accumulators)
-// with a running maximum and sum per row.  K rows are kept in LDS in the order (bits 2 and 3 of the position swapped) that makes a
-// lane's accumulators sixteen positions in two runs of eight: P's operand without a move between lanes.
-// fp32 queries and the probabilities beside them enter as three bf16 terms (24 bits); bf16 queries as they are, and the
-// probabilities rounded to bf16 (2^-9 each, independent: less than the output's own rounding).
+// Row r = (sequence * n_tok + token) * group + query head of a K / V head's rows.  A workgroup takes up to 128 rows (k_attn_many) or up to 16 or 32
+// (k_attn_few) of one K / V head and a range of positions, of the prompt (then the rows are those of all sequences) or of one sequence's own.
+//   S^T[position][row] = K . Q^T,   O^T[channel][row] += V^T . P^T       (32x32x16 or 16x16x32 bf16, fp32 accumulators)
+// with a running maximum and sum per row, in fp32.  K rows lie in LDS in the order that gives a lane the scores of consecutive positions, eight at a time: P's
+// operand without a move between lanes.  fp32 queries and the probabilities beside them enter as three bf16 terms (24 bits); bf16 queries as they are,
+// and the probabilities rounded to bf16 (relative error up to 2^-8 each, independent, so that a row's sum of many errs by less than its own rounding to
+// bf16; the sum that divides it is that of the unrounded ones).
 
 struct SoftParts { u32x4 t[3]; };
 
@@ -600,7 +604,10 @@ struct AttnPut {
   }
 };
 
-// 128 rows: four wavefronts of 32 that share the positions through LDS, 64 at a time in two buffers.
+// 128 rows: four wavefronts of 32 that share the positions through LDS, 64 at a time in two buffers.  Bound by the LDS reads of K and V beside the products (each
+// wavefront reads all of a tile: 128 KiB at 128 bytes a clock are as long as the products of two workgroups of a compute unit) and, in long prompts whose pages lie in
+// random order, by the feed: 96 sequences of 32 heads on 8 behind 65537 positions 122 us, 0.85 PFLOP/s; 4608 rows of one K / V head over 3001 positions 20 us,
+// one workgroup a compute unit (2.6 us for a tile, as with two).  Scores of the next tile between the products of this one in a wavefront: 123 to 130 us.
 template <int DH, bool F32>
 __device__ __forceinline__ void attn_many(const SharedAttnArgs& a, const AttnItem& it, char* lds) {
   typedef AttnBlock<DH> Bk;
@@ -663,7 +670,8 @@ __device__ __forceinline__ void attn_many(const SharedAttnArgs& a, const AttnIte
 
 // Up to RB rows: WT wavefronts take a block of 32 positions each in turn, copied by themselves into a K and a V buffer of their own (no barrier): the
 // next block's K is on its way from the scores on, its V from the output on, and other wavefronts of the SIMD cover what is left of the wait.
-// Results are put together at the end.  `also`: a second range for the same rows, walked first (pool == nullptr: none).
+// Results are put together at the end.  Bound by the feed: own positions of 96 sequences on 8 heads, 1 to 700 each, 137 MB, 49 us, 2.8 TB/s (ranges of equal length, sequences
+// of different ones); eight beams of 40 heads over 2048 + 130 positions, 54 MB, 16 us; four of 12 heads over 523 + 37 7 us, round trips.  `also`: a second range for the same rows, walked first (pool == nullptr: none).
 template <int DH, int RB, int WT, bool F32> struct FewShape {
   typedef AttnBlock<DH> Bk;
   static constexpr int OLD = DH + 4;                            // a row put together in LDS
@@ -832,7 +840,8 @@ __global__ __launch_bounds__(64 * WT, RB == 32 && DH == 128 ? 1 : 2) void k_attn
 }
 
 // The parts of a row put together.  DH / 4 lanes a row: first every lane takes statistics of some parts, then its four channels of all of them,
-// eight parts on their way at once.  Bound by the round trips: parts come from other XCDs' stores, through the memory-side cache.
+// eight parts on their way at once.  Bound by the round trips: parts come from other XCDs' stores, through the memory-side cache (3.6 us for 48 rows, 5.5 us for 4608 of
+// eight parts, 19 MB).
 template <int DH, bool F32>
 __global__ __launch_bounds__(256) void k_shared_merge(SharedAttnArgs a) {
   constexpr int LPR = DH / 4, RPW = 256 / LPR, PPL = ATTN_MAX_PARTS / LPR;
@@ -1191,7 +1200,7 @@ template <bool LONG>
 __global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
   extern __shared__ __align__(16) char smem[];
   __shared__ int s_bad;
-  __shared__ int s_n[DISCO_BEAM_MAX_ROWS];
+  __shared__ int s_n[DISCO_BEAM_MAX_ROWS], s_cut[DISCO_BEAM_MAX_ROWS];         // candidates of a row, and those that can be wanted
   const int g = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6, nw = blockDim.x >> 6, k = a.k;
   const float per_unit = 1.0f / (float)a.units;
   BeamCand* cand = reinterpret_cast<BeamCand*>(smem);
@@ -1243,7 +1252,14 @@ __global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) q[e & 3] = max(q[e & 3], (uint32_t)(r[e] >> 32));
         const uint32_t bound = kth_bound(q, k);
-        if constexpr (LONG) wave_top_k_memory(src, total, bound, k, list, keys);
+        bool deep = false;                                      // the last of a unit's in registers reaches the bound: there may be more behind it
+        if constexpr (LONG) {
+          const int last = 64 * 16 / a.units - 1;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) deep |= (uint32_t)(r[e] >> 32) >= max(bound, 1u) && part(e * 64 + lane, per_unit) == last;
+          deep = __any(deep);
+        }
+        if (LONG && deep) wave_top_k_memory(src, total, bound, k, list, keys);
         else wave_top_k_keys(r, bound, k, list, keys);
         wave_lds_fence();
         for (int i = lane; i < k; i += 64) {
@@ -1260,15 +1276,24 @@ __global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
   const bool bad = s_bad != 0;
   int have = 0;
   for (int b = 0; b < a.n_beams; ++b) have += s_n[b];
-  // rank of every candidate: its place in its own row's list and, counted row by row, the better ones of the others (lists in order)
+  // Rank of a candidate: its place in its own row's list and, counted row by row, the better ones of the others (lists in order).  LONG: every eighth of
+  // a list first, behind one that has k better ones no other is wanted; neighbouring lanes take the same place of different rows, so that places that
+  // are not wanted are skipped by whole wavefronts (32 beams of 64 candidates: 12 us less; four beams of four: 0.1 us more).
   const int n_all = a.n_beams * k;
-  const float per_beam = 1.0f / (float)k, per_set = 1.0f / (float)n_all;
+  const float per_beam = 1.0f / (float)k, per_row = 1.0f / (float)a.n_beams;
   for (int i = t; i < n_all; i += blockDim.x) cand[i].rank = i - part(i, per_beam) * k;
+  for (int b = t; b < a.n_beams; b += blockDim.x) s_cut[b] = s_n[b];
   __syncthreads();
-  if (!bad)
-    for (int i = t; i < n_all * a.n_beams; i += blockDim.x) {
-      const int o = part(i, per_set), c = i - o * n_all, b = part(c, per_beam);
-      if (o == b || c - b * k >= s_n[b]) continue;
+  auto count = [&](const int step, const bool rest) {
+    const int n_p = (k + step - 1) / step, n_set = n_p * a.n_beams;
+    const float per_set = 1.0f / (float)n_set;
+    for (int i = t; i < n_set * a.n_beams; i += blockDim.x) {
+      const int o = part(i, per_set), x = i - o * n_set;
+      int b, p;
+      if constexpr (LONG) { const int place = part(x, per_row); b = x - place * a.n_beams; p = place * step; }
+      else { b = part(x, per_beam); p = x - b * k; }
+      if (o == b || p >= s_cut[b] || (rest && (p & 7) == 0)) continue;
+      const int c = b * k + p;
       const double mine = cand[c].s;
       int lo = 0, hi = s_n[o];
       while (lo < hi) {
@@ -1278,11 +1303,23 @@ __global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
       }
       if (lo > 0) atomicAdd(&cand[c].rank, lo);
     }
-  __syncthreads();
+    __syncthreads();
+  };
+  if (!bad) {
+    if constexpr (LONG) {
+      count(8, false);
+      for (int i = t; i < n_all; i += blockDim.x) {
+        const int b = part(i, per_beam), p = i - b * k;
+        if ((p & 7) == 0 && p < s_n[b] && cand[i].rank >= k) atomicMin(&s_cut[b], p);
+      }
+      __syncthreads();
+    }
+    count(1, LONG);
+  }
   for (int i = t; i < n_all; i += blockDim.x) {
     const int b = part(i, per_beam);
     const BeamCand c = cand[i];
-    if (bad || i - b * k >= s_n[b] || c.rank >= k) continue;
+    if (bad || i - b * k >= s_cut[b] || c.rank >= k) continue;
     const size_t at = (size_t)g * k + c.rank;
     a.tokens[at] = c.token; a.parents[at] = b; a.scores_out[at] = (float)c.s;
     if (a.done_out != nullptr) a.done_out[at] = (a.done != nullptr && a.done[g * a.n_beams + b] != 0) || c.token == a.end_token ? 1 : 0;
@@ -1301,7 +1338,8 @@ __global__ __launch_bounds__(1024) void k_beam_merge(BeamSelectArgs a) {
 // Sequence b of a group goes on from sequence parents[b].  Pages that are full are shared by reference; of the one being filled
 // the first child takes its parent's, further children get those of sequences without a child, with the contents copied.
 // Workgroups: `pieces` of every copied page of every layer (a sequence that needs no copy ends at once), then one for the group's tables.
-// Bound by the copies: 16 bytes a lane, four at a time.
+// Bound by the copies: 16 bytes a lane, four at a time (48 pages of 16 positions of 8 heads of 128 in 16 layers, 101 MB: 23 us, 4.3 TB/s; 40 layers of one beam's page of
+// 40 heads, 26 MB: 8.7 us).
 __global__ __launch_bounds__(256) void k_beam_reorder(BeamReorderArgs a, int pieces) {
   __shared__ int s_par[64], s_dst[64], s_src[64], s_of[64], s_n;
   const int nb = a.n_beams, t = threadIdx.x, g = blockIdx.y;
